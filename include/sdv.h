@@ -419,6 +419,121 @@ int sdv_last_verify_ms(sdv_ctx *ctx, float *ms);
 int sdv_gemm_noalloc(const float *dev_x, const uint16_t *dev_w, float *dev_y, int M, int N, int K,
                      void *cuda_stream);
 
+/* ---- Operators on a cache kept in pages -------------------------------------------------------------
+ * For callers who serve several sequences from one pool of pages and run the dense layers themselves: the parts of a
+ * speculative step (paper Sec. 3.2, Sec. 4.1) as calls of their own, without a context.  The paper has no counterpart of
+ * pages or of sampling.  In the order of a step:
+ *   sdv_paged_slots      hands pages to the sequences that need more, gives every row its position and its slot
+ *   sdv_rope_append      rotates queries and keys by their positions, writes keys and values to their slots
+ *   sdv_tree_attention   every row attends to its sequence's cache and to its own path through the draft tree
+ *   sdv_verify_sampled   accepts drafts against the target model's probabilities, samples one more token
+ * A sequence's rows are row 0, the committed token, and its drafts.  The rows of all sequences lie one behind the other:
+ * sequence b has rows cu_rows[b] <= r < cu_rows[b + 1] (device int32 [n_seqs + 1], ascending from 0, at most n_rows).
+ * parent[r] (device int32 [n_rows], or NULL: a chain) is the row of the same sequence, counted from its row 0, that row r
+ * continues; of row 0 it is not read, and a value that is not in [0, r - cu_rows[b]) counts as 0, as in sdv_verify_tree.
+ * kv_len[b] is the number of committed tokens; row i of a sequence lies at token kv_len[b] + i of its cache, at position
+ * kv_len[b] + its depth in the tree.  Token t of a sequence is token t % page_size of page block_table[b][t / page_size];
+ * slot s of the pool is token s % page_size of page s / page_size.
+ *
+ * All of these calls only queue work on cuda_stream (NULL: the default stream) of the current device and return: they can be
+ * captured into a graph, from the second call on each device on (the first one loads code).  They allocate nothing and keep
+ * nothing between calls.  Pointers are checked on the host (alignment; device memory of the current device), sizes too; what
+ * lies in device memory is not: the kernels stay within the buffers whatever it holds, as each call says.  Calls
+ * that share no output and no workspace may run at the same time.  n_seqs is at most SDV_MAX_SEQUENCES; except for
+ * sdv_paged_slots, calls without sequences or rows do nothing.  Errors: SDV_EINVAL, SDV_ENOMEM (workspace), SDV_ECUDA. */
+#define SDV_MAX_SEQUENCES 4096
+#define SDV_TREE_ROWS 64  /* rows of a sequence that sdv_tree_attention and sdv_verify_sampled take */
+
+enum { SDV_BF16 = 0, SDV_FP16 = 1 };
+
+/* Keys and values of one layer in pages: element d of token t of KV head h of page p at k[p * page_stride + h * head_stride +
+ * t * token_stride + d] (strides in elements; the same for v).  Both 16-byte aligned, strides multiples of 8. */
+typedef struct {
+    void *k, *v;
+    int dtype;   /* SDV_BF16 or SDV_FP16 */
+    int n_pages, page_size, n_kv_heads, head_dim;
+    long long page_stride, head_stride, token_stride;
+} sdv_pages;
+
+/* Block tables and slots from the sequences' lengths.  Sequence b needs ceil((kv_len[b] + its rows) / page_size) pages (none
+ * without rows) and holds the first n_held[b] entries of its row of block_table; the missing ones are taken from free_pages, sequence by
+ * sequence, from entry free_state[0] on, and written behind those it holds.  A sequence whose pages do not fit its row of the
+ * table, or that comes when the list has run out, is refused: it gets no page and its rows' slots are -1.  Out: slots and
+ * positions of all rows (rows that belong to no sequence: slot -1, position 0), the pages held from now on, and free_state_out =
+ * {first unused entry of free_pages, sequences refused}.  Out arrays must not be in arrays.  Entries of block_table and free_pages are
+ * not checked against the pool (sdv_rope_append and sdv_tree_attention do that); a negative one gives slot -1. */
+typedef struct {
+    const int32_t *kv_len, *cu_rows, *parent, *n_held, *free_pages, *free_state;
+    int32_t *block_table;   /* [n_seqs][table_width], rows table_stride apart; updated */
+    int32_t *slots, *positions, *n_held_out, *free_state_out /* [2] */;
+    long long table_stride;
+    int n_seqs, n_rows, page_size, table_width, n_free;
+} sdv_slots_args;
+int sdv_paged_slots(const sdv_slots_args *a, void *cuda_stream);
+
+/* Rotary embedding with cache append.  Pair i < rot_dim / 2 of a head of q and of k, its elements i and i + rot_dim / 2, or 2i and
+ * 2i + 1 when interleaved, is rotated by the angle positions[r] * frequencies[i] (in 64 bits, any int32 position) and scaled by
+ * `factor`; elements from rot_dim on pass through.  Computed in 32 bits, rounded once.  q goes to q_out (may be q, with the same strides), k
+ * and v go to slot slots[r] of `pages`; a row whose slot is outside the pool (as -1) is not written.  q, or k and v, may be NULL. Of rows that share
+ * a slot any one may stay.  rot_dim even, 0 < rot_dim <= head_dim <= 256, head_dim even; any strides, elements of a head contiguous.
+ * Accepted rows of a tree reach their consecutive places the same way: the same k, v and positions again, with q NULL and the slots that
+ * sdv_verify_sampled gives. */
+typedef struct {
+    const void *q, *k, *v;
+    void *q_out;
+    const int32_t *positions, *slots;
+    const double *frequencies;   /* device [rot_dim / 2] */
+    long long q_row_stride, q_head_stride, out_row_stride, out_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+    int n_rows, n_q_heads, n_kv_heads, head_dim, rot_dim, interleaved, dtype;
+    float factor;
+} sdv_rope_args;
+int sdv_rope_append(const sdv_rope_args *a, const sdv_pages *pages /* NULL without k */, void *cuda_stream);
+
+/* Attention of every row over tokens [0, kv_len[b]) of its sequence and over the tokens of the rows on its own path (itself included),
+ * which have been appended before: out = softmax(scale * q k^T) v, query head h with KV head h / (n_q_heads / n_kv_heads).  head_dim 64 or
+ * 128, page_size a power of two from 8 on, scale > 0.  Scores, statistics and sums in fp32, probabilities rounded to the 16-bit
+ * type for the second product.  What lies in places that a row may not see, infinities and NaN too, does not reach it.  Tokens past
+ * table_width * page_size are left out; entries of block_table outside the pool read as zeros.  Rows of a sequence past
+ * SDV_TREE_ROWS and rows of no sequence are left as they were in `out`.  `workspace`: sdv_tree_attention_workspace_bytes bytes, 256-byte
+ * aligned, contents free before and after; calls that may run at the same time need one each.  status (may be NULL): set to 1 when a wait inside
+ * the kernel ran out, which leaves NaN in the rows concerned; never cleared. */
+typedef struct {
+    const void *q;
+    void *out;
+    const int32_t *block_table, *kv_len, *cu_rows, *parent;
+    void *workspace;
+    int32_t *status;
+    size_t workspace_bytes;
+    long long q_row_stride, q_head_stride, out_row_stride, out_head_stride, table_stride;
+    int n_seqs, n_rows, n_q_heads, table_width;
+    float scale;
+} sdv_attention_args;
+size_t sdv_tree_attention_workspace_bytes(int n_seqs, int head_dim);
+int sdv_tree_attention(const sdv_attention_args *a, const sdv_pages *pages, void *cuda_stream);
+
+/* Verification of drafted tokens against the target's probabilities, with the caller's random numbers u[r] in [0, 1).  target[r] is the target
+ * model's distribution behind row r.
+ *   With draft[r], the distribution that row r's token x was sampled from (chains only): row r is accepted when u[r] * draft[r][x] <
+ *   target[row before][x]; behind the first rejected row the next token is drawn from max(target - draft, 0).
+ *   Without (retrieved drafts, which are certain): the children of the last accepted row are looked at in ascending order; one
+ *   is accepted when u[r] * (1 - the target's shares of the tokens rejected before it) < target[x], a token rejected before having no share;
+ *   when none is, the next token is drawn from the target's distribution without the rejected tokens.
+ * This leaves the target's distribution unchanged.  Drawn: the smallest token whose cumulative sum exceeds u[row 0] * the whole sum, in 64 bits; where nothing is left, from the
+ * target's distribution itself, and -1 where that holds nothing either.  Values that are not positive have no share.  Tokens outside the vocabulary are
+ * rejected.  Out: accept_len[b] (-1: no rows); out_tokens, from entry cu_rows[b] on, the accept_len[b] accepted tokens and the drawn one; out_rows
+ * likewise row 0 and the accepted rows, counted from row 0; -1 behind them and for rows of no sequence.  With slots (each row's, from sdv_paged_slots):
+ * out_slots[r], where an accepted row's keys and values belong once the others are dropped, -1 for rows that are dropped or lie
+ * there already.  Rows past SDV_TREE_ROWS are not looked at.  Probabilities are fp32; row strides in elements. */
+typedef struct {
+    const float *target, *draft;
+    const int32_t *tokens, *cu_rows, *parent, *slots;
+    const float *uniforms;
+    int32_t *accept_len, *out_tokens, *out_rows, *out_slots;
+    long long target_stride, draft_stride;
+    int n_seqs, n_rows, vocab;
+} sdv_verify_args;
+int sdv_verify_sampled(const sdv_verify_args *a, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

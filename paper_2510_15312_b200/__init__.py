@@ -7,6 +7,8 @@ does not.
 """
 from .binding import (SdvError, Sdv, SdvConfig, lib, load_library, EXPORTS, OK, EINVAL, ENOMEM, ECAPACITY,
                       ESTATE, ECUDA, ETIMEOUT, ETOOBIG, gemm_noalloc)
+from .paged import paged_slots, rope_append, rope_frequencies, tree_attention, tree_attention_workspace, verify_sampled
 
 __all__ = ["SdvError", "Sdv", "SdvConfig", "lib", "load_library", "EXPORTS", "OK", "EINVAL", "ENOMEM",
-           "ECAPACITY", "ESTATE", "ECUDA", "ETIMEOUT", "ETOOBIG", "gemm_noalloc"]
+           "ECAPACITY", "ESTATE", "ECUDA", "ETIMEOUT", "ETOOBIG", "gemm_noalloc", "paged_slots", "rope_append", "rope_frequencies", "tree_attention",
+           "tree_attention_workspace", "verify_sampled"]

@@ -24,6 +24,7 @@ EXPORTS = [
     "sdv_debug_top_successors",
     "sdv_follower_workspace_bytes", "sdv_create_follower", "sdv_verify_batch", "sdv_get_verified",
     "sdv_decode_steps", "sdv_run_kernel_ms", "sdv_step",
+    "sdv_paged_slots", "sdv_rope_append", "sdv_tree_attention_workspace_bytes", "sdv_tree_attention", "sdv_verify_sampled",
 ]
 
 
@@ -114,8 +115,14 @@ def load_library(path: Optional[str] = None):
     L.sdv_verify_tree.argtypes = [vp, i32p, i32p, C.c_int, i32p, i32p, ip]
     L.sdv_debug_force_commit_tree.argtypes = [vp, i32p, C.c_int, C.c_int]
     L.sdv_debug_top_successors.argtypes = [vp, vp, C.c_int, C.c_int, vp]
+    L.sdv_paged_slots.argtypes = [vp, vp]
+    L.sdv_rope_append.argtypes = [vp, vp, vp]
+    L.sdv_tree_attention_workspace_bytes.argtypes = [C.c_int, C.c_int]
+    L.sdv_tree_attention_workspace_bytes.restype = C.c_size_t
+    L.sdv_tree_attention.argtypes = [vp, vp, vp]
+    L.sdv_verify_sampled.argtypes = [vp, vp]
     for name in EXPORTS:
-        if name not in ("sdv_workspace_bytes", "sdv_follower_workspace_bytes", "sdv_strerror", "sdv_launch_count"):
+        if name not in ("sdv_workspace_bytes", "sdv_follower_workspace_bytes", "sdv_tree_attention_workspace_bytes", "sdv_strerror", "sdv_launch_count"):
             getattr(L, name).restype = C.c_int
     _lib = L
     return L

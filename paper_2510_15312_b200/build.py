@@ -6,7 +6,9 @@ import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsdv.so")
-_SOURCES = ["sdv.cu", "forward.cuh", "dense.cuh", "device_once.h", "layout.cuh", "ptx.cuh", "small_gemm.cuh", "small_kernels.cuh"]
+_UNITS = ["sdv.cu", "paged.cu"]   # compiled side by side
+_SOURCES = _UNITS + ["forward.cuh", "dense.cuh", "device_once.h", "layout.cuh", "paged.cuh", "ptx.cuh", "small_gemm.cuh", "small_kernels.cuh",
+                     "tensor_map.h", "tree_attention.cuh", "tree_plan.h", "verify_sampled.cuh"]
 
 
 HASH_PATH = LIB_PATH + ".srchash"
@@ -35,13 +37,18 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB_PATH
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo",
-           "-shared", "-Xcompiler", "-fPIC", "-o", LIB_PATH + ".tmp", os.path.join(_HERE, "csrc", "sdv.cu")]
+    flags = [nvcc, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-Xcompiler", "-fPIC"]
     if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-        print(" ".join(cmd))
-    subprocess.run(cmd, check=True)
+        flags[1:1] = ["-Xptxas", "-v"]
+    objects = [os.path.join(_HERE, "csrc", u[:-3] + ".o") for u in _UNITS]
+    commands = [flags + ["-c", "-o", o, os.path.join(_HERE, "csrc", u)] for u, o in zip(_UNITS, objects)]
+    if verbose:
+        print("\n".join(" ".join(c) for c in commands))
+    running = [subprocess.Popen(c) for c in commands]
+    for p, c in [(p, p.wait()) for p in running]:
+        if c:
+            raise subprocess.CalledProcessError(c, p.args)
+    subprocess.run([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", LIB_PATH + ".tmp"] + objects, check=True)
     os.replace(LIB_PATH + ".tmp", LIB_PATH)
     with open(HASH_PATH, "w") as fh:
         fh.write(_source_hash())

@@ -1,0 +1,291 @@
+// C entry points of the operators on a cache kept in pages (see include/sdv.h): checks of the arguments and launches.
+#include "../../include/sdv.h"
+
+#include <cuda_runtime.h>
+#include <math.h>
+#include <string.h>
+
+#include <initializer_list>
+
+#include "device_once.h"
+#include "paged.cuh"
+#include "tensor_map.h"
+#include "tree_attention.cuh"
+#include "verify_sampled.cuh"
+
+using namespace sdv;
+
+namespace {
+
+constexpr int kMaxVocab = 1 << 21;   // tile sums of a block of sdv_verify_sampled stay within 32 KB
+
+// Device memory of the current device (where the runtime can tell), on a boundary of `align` bytes.
+bool on_device(const void* p, int dev, size_t align) {
+    if (!p || ((uintptr_t)p & (align - 1))) return false;
+    cudaPointerAttributes at;
+    if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == dev);
+}
+bool on_device(std::initializer_list<const void*> ps, int dev, size_t align) {
+    for (const void* p : ps)
+        if (!on_device(p, dev, align)) return false;
+    return true;
+}
+
+int sm_count(int dev) {
+    static std::atomic<int> known[64];
+    if (dev < 0 || dev >= 64) return 0;
+    int n = known[dev].load(std::memory_order_relaxed);
+    if (!n && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) known[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+// A launch, in clusters of `cluster` blocks, `dependent`: one that may overlap the tail of the kernel before it.
+template <typename... KArgs, typename... Args>
+int launch(void (*kernel)(KArgs...), int grid, int block, size_t smem, void* stream, int cluster, bool dependent, const Args&... args) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute at[2];
+    int n = 0;
+    if (cluster > 1) {
+        at[n].id = cudaLaunchAttributeClusterDimension;
+        at[n].val.clusterDim.x = (unsigned)cluster;
+        at[n].val.clusterDim.y = 1;
+        at[n++].val.clusterDim.z = 1;
+    }
+    if (dependent) {
+        at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    cfg.attrs = at;
+    cfg.numAttrs = (unsigned)n;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? SDV_OK : SDV_ECUDA;
+}
+
+bool pages_ok(const sdv_pages* p, int dev) {
+    if (!p || (p->dtype != SDV_BF16 && p->dtype != SDV_FP16)) return false;
+    if (p->n_pages < 1 || p->page_size < 1 || p->n_kv_heads < 1 || p->head_dim < 1 || (long long)p->n_pages * p->page_size > INT_MAX) return false;
+    if (p->page_stride < 0 || p->head_stride < 0 || p->token_stride < 0 || ((p->page_stride | p->head_stride | p->token_stride) & 7)) return false;
+    return on_device(p->k, dev, 16) && on_device(p->v, dev, 16);
+}
+
+typedef void (*RopeKernel)(const sdv_rope_args, const sdv_pages, int);
+template <typename T, bool I>
+RopeKernel rope_kernel(int w) {
+    return w == 8 ? rope_append_kernel<T, I, 8> : w == 4 ? rope_append_kernel<T, I, 4> : w == 2 ? rope_append_kernel<T, I, 2> : rope_append_kernel<T, I, 1>;
+}
+RopeKernel rope_kernel(int dtype, bool interleaved, int w) {
+    if (dtype == SDV_BF16) return interleaved ? rope_kernel<__nv_bfloat16, true>(w) : rope_kernel<__nv_bfloat16, false>(w);
+    return interleaved ? rope_kernel<__half, true>(w) : rope_kernel<__half, false>(w);
+}
+
+typedef void (*TreeKernel)(const CUtensorMap, const CUtensorMap, const TreeParams);
+typedef void (*MergeKernel)(const TreeParams, int);
+TreeKernel tree_kernel(int dtype, int hd) {
+    if (dtype == SDV_BF16) return hd == 128 ? tree_attention_kernel<__nv_bfloat16, 128> : tree_attention_kernel<__nv_bfloat16, 64>;
+    return hd == 128 ? tree_attention_kernel<__half, 128> : tree_attention_kernel<__half, 64>;
+}
+MergeKernel merge_kernel(int dtype, int hd) {
+    if (dtype == SDV_BF16) return hd == 128 ? tree_merge_kernel<__nv_bfloat16, 128> : tree_merge_kernel<__nv_bfloat16, 64>;
+    return hd == 128 ? tree_merge_kernel<__half, 128> : tree_merge_kernel<__half, 64>;
+}
+size_t tree_smem(int hd) { return hd == 128 ? TreeShape<128>::kSmemBytes : TreeShape<64>::kSmemBytes; }
+
+// Code of every kernel is loaded, and the attention's shared memory allowed, by the first call on a device.
+int prepare_device(int dev) {
+    static DeviceOnce once;
+    const cudaError_t e = once.run(dev, []() {
+        cudaError_t r = cudaSuccess;
+        cudaFuncAttributes fa;
+        const auto load = [&](const void* f) { if (r == cudaSuccess) r = cudaFuncGetAttributes(&fa, f); };
+        load((const void*)paged_slots_kernel);
+        load((const void*)verify_sampled_kernel);
+        for (int t = SDV_BF16; t <= SDV_FP16; ++t) {
+            for (int w = 1; w <= 8; w *= 2)
+                for (int i = 0; i < 2; ++i) load((const void*)rope_kernel(t, i != 0, w));
+            for (int hd = 64; hd <= 128; hd += 64) {
+                load((const void*)merge_kernel(t, hd));
+                if (r == cudaSuccess) r = cudaFuncSetAttribute((const void*)tree_kernel(t, hd), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tree_smem(hd));
+            }
+        }
+        return r;
+    });
+    return e == cudaSuccess ? SDV_OK : SDV_ECUDA;
+}
+
+// Keys (or values) as a tensor of head_dim x tokens of a page x KV heads x pages; boxes of 64 x box_keys elements, 128-byte swizzle, zeros outside.
+bool make_page_map(CUtensorMap* m, const void* base, const sdv_pages* p, int box_keys) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const auto stride = [](int n, long long s) { return (cuuint64_t)(n > 1 && s ? s * 2 : 16); };   // of a dimension of one: anything valid
+    const cuuint64_t dims[4] = {(cuuint64_t)p->head_dim, (cuuint64_t)p->page_size, (cuuint64_t)p->n_kv_heads, (cuuint64_t)p->n_pages};
+    const cuuint64_t strides[3] = {stride(p->page_size, p->token_stride), stride(p->n_kv_heads, p->head_stride), stride(p->n_pages, p->page_stride)};
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_keys, 1, 1}, estr[4] = {1, 1, 1, 1};
+    return fn(m, p->dtype == SDV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+int tree_blocks(int dev) { return min(kTreeBlocksPerSm * sm_count(dev), kTreeMaxBlocks); }
+// Workspace: tiles before every sequence | maxima and sums | outputs.
+size_t tree_bytes(int n_seqs, int head_dim, int blocks, int rows) {
+    const size_t parts = (size_t)blocks * 2 * rows;
+    return align256(((size_t)n_seqs + 1) * sizeof(long long)) + align256(parts * sizeof(float2)) + parts * head_dim * sizeof(float);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sdv_paged_slots(const sdv_slots_args* a, void* cuda_stream) {
+    if (!a || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->page_size < 1 || a->table_width < 0 || a->n_free < 0) return SDV_EINVAL;
+    if (a->table_stride < a->table_width && a->n_seqs > 1) return SDV_EINVAL;
+    if ((long long)a->n_seqs * a->table_width > INT_MAX) return SDV_EINVAL;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;
+    if (!on_device({a->cu_rows, a->free_state, a->free_state_out}, dev, 4)) return SDV_EINVAL;
+    if (a->n_seqs && !on_device({a->kv_len, a->n_held, a->n_held_out}, dev, 4)) return SDV_EINVAL;
+    if (a->n_seqs && a->table_width && !on_device(a->block_table, dev, 4)) return SDV_EINVAL;
+    if (a->n_free && !on_device(a->free_pages, dev, 4)) return SDV_EINVAL;
+    if (a->n_rows && (!on_device({a->slots, a->positions}, dev, 4) || (a->parent && !on_device(a->parent, dev, 4)))) return SDV_EINVAL;
+    // every block reads what these hold at the start
+    if ((a->n_seqs && a->n_held_out == a->n_held) || a->free_state_out == a->free_state) return SDV_EINVAL;
+    const int rc = prepare_device(dev);
+    if (rc != SDV_OK) return rc;
+    const long long items = (long long)a->n_rows + min((long long)a->n_free, (long long)a->n_seqs * a->table_width);
+    const int grid = (int)max(1ll, min((items + kSlotThreads - 1) / kSlotThreads, (long long)sm_count(dev)));
+    return launch(paged_slots_kernel, grid, kSlotThreads, 0, cuda_stream, 1, false, *a);
+}
+
+int sdv_rope_append(const sdv_rope_args* a, const sdv_pages* pages, void* cuda_stream) {
+    if (!a || a->n_rows < 0 || (a->dtype != SDV_BF16 && a->dtype != SDV_FP16)) return SDV_EINVAL;
+    if (a->head_dim < 2 || a->head_dim > 256 || a->head_dim % 2 || a->rot_dim < 2 || a->rot_dim > a->head_dim || a->rot_dim % 2) return SDV_EINVAL;
+    if ((!a->k) != (!a->v) || (!a->q && !a->k) || (a->q && a->n_q_heads < 1) || (a->k && a->n_kv_heads < 1)) return SDV_EINVAL;
+    if (a->n_rows == 0) return SDV_OK;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;
+    if (!on_device(a->positions, dev, 4) || !on_device(a->frequencies, dev, 8)) return SDV_EINVAL;
+    uintptr_t bits = 0;   // what the addresses of a row have in common, in elements
+    if (a->q) {
+        if (!on_device({a->q, a->q_out}, dev, 2)) return SDV_EINVAL;
+        bits |= (uintptr_t)a->q >> 1 | (uintptr_t)a->q_out >> 1 | (uintptr_t)(a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride);
+    }
+    sdv_pages none;
+    memset(&none, 0, sizeof(none));
+    none.page_size = 1;
+    if (a->k) {
+        if (!on_device({a->k, a->v}, dev, 2) || !on_device(a->slots, dev, 4) || !pages_ok(pages, dev)) return SDV_EINVAL;
+        if (pages->dtype != a->dtype || pages->n_kv_heads != a->n_kv_heads || pages->head_dim != a->head_dim) return SDV_EINVAL;
+        bits |= (uintptr_t)a->k >> 1 | (uintptr_t)a->v >> 1 | (uintptr_t)(a->k_row_stride | a->k_head_stride | a->v_row_stride | a->v_head_stride);
+    }
+    const int rc = prepare_device(dev);
+    if (rc != SDV_OK) return rc;
+    // elements moved at once: as many as the pairs' two halves, the strides and the addresses allow
+    const int half = a->rot_dim / 2;
+    int w = 8;
+    while (w > 1 && (half % w || a->head_dim % (2 * w) || (bits & (uintptr_t)(w - 1)))) w /= 2;
+    const int tokens = max(1, min(8, a->n_rows / (sm_count(dev) * 8)));
+    return launch(rope_kernel(a->dtype, a->interleaved != 0, w), (a->n_rows + tokens - 1) / tokens, kRopeThreads, (size_t)tokens * half * sizeof(float2), cuda_stream, 1, false, *a,
+                  a->k ? *pages : none, tokens);
+}
+
+size_t sdv_tree_attention_workspace_bytes(int n_seqs, int head_dim) {
+    int dev = 0;
+    if (n_seqs < 0 || n_seqs > SDV_MAX_SEQUENCES || (head_dim != 64 && head_dim != 128) || cudaGetDevice(&dev) != cudaSuccess) return 0;
+    return tree_bytes(n_seqs, head_dim, tree_blocks(dev), kTreeTileRows);
+}
+
+int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void* cuda_stream) {
+    if (!a || !pages || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->table_width < 0) return SDV_EINVAL;
+    if (pages->head_dim != 64 && pages->head_dim != 128) return SDV_EINVAL;
+    if (pages->page_size < 8 || (pages->page_size & (pages->page_size - 1)) || pages->n_kv_heads < 1) return SDV_EINVAL;
+    if (a->n_q_heads < 1 || a->n_q_heads % pages->n_kv_heads || !(a->scale > 0.f) || !isfinite(a->scale)) return SDV_EINVAL;
+    if (a->table_stride < a->table_width && a->n_seqs > 1) return SDV_EINVAL;
+    if ((a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride) & 7) return SDV_EINVAL;
+    if (a->n_seqs == 0 || a->n_rows == 0 || a->table_width == 0) return SDV_OK;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;
+    if (!pages_ok(pages, dev) || !on_device({a->q, a->out}, dev, 16) || !on_device({a->block_table, a->kv_len, a->cu_rows}, dev, 4)) return SDV_EINVAL;
+    if ((a->parent && !on_device(a->parent, dev, 4)) || (a->status && !on_device(a->status, dev, 4)) || !on_device(a->workspace, dev, 256)) return SDV_EINVAL;
+    const int rc = prepare_device(dev);
+    if (rc != SDV_OK) return rc;
+
+    TreeParams P;
+    memset(&P, 0, sizeof(P));
+    const int hd = pages->head_dim, g = a->n_q_heads / pages->n_kv_heads;
+    const long long rows = (long long)min(a->n_rows, SDV_TREE_ROWS) * g, chunks = (rows + kTreeTileRows - 1) / kTreeTileRows;
+    const long long keys = min((long long)a->table_width * pages->page_size, (long long)INT_MAX);
+    const long long most = ((keys + kTreeKeys - 1) / kTreeKeys) * chunks * pages->n_kv_heads * min(a->n_seqs, a->n_rows);   // no more tiles than this
+    P.blocks = (int)min((long long)tree_blocks(dev), most);
+    P.part_rows = (int)min(rows, (long long)kTreeTileRows);
+    if (a->workspace_bytes < tree_bytes(a->n_seqs, hd, P.blocks, P.part_rows)) return SDV_ENOMEM;
+    const size_t parts = (size_t)P.blocks * 2 * P.part_rows;
+    uint8_t* ws = (uint8_t*)a->workspace;
+    P.tiles_before = (long long*)ws;
+    ws += align256(((size_t)a->n_seqs + 1) * sizeof(long long));
+    P.part_ml = (float2*)ws;
+    P.part_o = (float*)(ws + align256(parts * sizeof(float2)));
+    P.q = a->q;
+    P.out = a->out;
+    P.v = pages->v;
+    P.block_table = a->block_table;
+    P.kv_len = a->kv_len;
+    P.cu_rows = a->cu_rows;
+    P.parent = a->parent;
+    P.status = a->status;
+    P.q_row_stride = a->q_row_stride;
+    P.q_head_stride = a->q_head_stride;
+    P.out_row_stride = a->out_row_stride;
+    P.out_head_stride = a->out_head_stride;
+    P.table_stride = a->table_stride;
+    P.page_stride = pages->page_stride;
+    P.head_stride = pages->head_stride;
+    P.token_stride = pages->token_stride;
+    P.n_seqs = a->n_seqs;
+    P.n_rows = a->n_rows;
+    P.n_kv = pages->n_kv_heads;
+    P.g = g;
+    P.table_width = a->table_width;
+    P.page_size = pages->page_size;
+    while ((1 << P.page_shift) < pages->page_size) ++P.page_shift;
+    P.n_pages = pages->n_pages;
+    P.scale_log2e = a->scale * 1.4426950408889634f;
+    P.wait_limit_ns = 2000000000ull;
+    CUtensorMap map_k, map_v;
+    const int box_keys = min(pages->page_size, kTreeKeys);
+    if (!make_page_map(&map_k, pages->k, pages, box_keys) || !make_page_map(&map_v, pages->v, pages, box_keys)) return SDV_EINVAL;
+    const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, false, map_k, map_v, P);
+    if (first != SDV_OK || P.blocks == 1) return first;   // one block does everything alone
+    // pairs of row and head that a merging block takes at a time: one while there are blocks to spare
+    const long long pairs = (long long)a->n_rows * a->n_q_heads, room = (long long)sm_count(dev) * 8;
+    const int group = (int)min((long long)kMergeWarps, (pairs + room - 1) / room);
+    return launch(merge_kernel(pages->dtype, hd), (int)min((pairs + group - 1) / group, room), kMergeThreads, 0, cuda_stream, 1, true, P, group);
+}
+
+int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {
+    if (!a || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->vocab < 1 || a->vocab > kMaxVocab) return SDV_EINVAL;
+    if ((a->draft && a->parent) || (!a->slots) != (!a->out_slots)) return SDV_EINVAL;
+    if (a->target_stride < a->vocab || (a->draft && a->draft_stride < a->vocab)) return SDV_EINVAL;
+    if (a->n_seqs == 0 || a->n_rows == 0) return SDV_OK;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;
+    if (!on_device({a->target, a->tokens, a->cu_rows, a->uniforms, a->accept_len, a->out_tokens, a->out_rows}, dev, 4)) return SDV_EINVAL;
+    if ((a->draft && !on_device(a->draft, dev, 4)) || (a->parent && !on_device(a->parent, dev, 4)) || (a->slots && !on_device({a->slots, a->out_slots}, dev, 4))) return SDV_EINVAL;
+    const int rc = prepare_device(dev);
+    if (rc != SDV_OK) return rc;
+    // blocks that share a sequence's vocabulary: doubled while every warp keeps a tile and about four blocks an SM are not exceeded
+    const int tiles = (a->vocab + kVerifyTile - 1) / kVerifyTile;
+    int cs = 1;
+    while (cs < kVerifyMaxCluster && tiles >= 2 * cs * kVerifyWarps && (long long)a->n_seqs * cs * 2 <= 4ll * sm_count(dev)) cs *= 2;
+    const int per = (tiles + cs - 1) / cs;
+    return launch(verify_sampled_kernel, a->n_seqs * cs, kVerifyThreads, (size_t)per * sizeof(double), cuda_stream, cs, false, *a, per);
+}
+
+}  // extern "C"

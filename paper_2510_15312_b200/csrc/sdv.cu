@@ -18,6 +18,7 @@
 #include "layout.cuh"
 #include "small_gemm.cuh"
 #include "small_kernels.cuh"
+#include "tensor_map.h"
 
 using namespace sdv;
 
@@ -563,23 +564,6 @@ int commit_common(sdv_ctx* ctx, int max_emit, int force_accept, int force_token,
 }
 
 // ---- dense prefill path (csrc/dense.cuh)
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled_fn() {
-    static std::atomic<EncodeTiledFn> fn{nullptr};   // the same for every thread and device
-    EncodeTiledFn known = fn.load(std::memory_order_acquire);
-    if (!known) {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess) {
-            known = (EncodeTiledFn)p;
-            fn.store(known, std::memory_order_release);
-        }
-    }
-    return known;
-}
 // bf16 matrix [rows][K] row-major on this GPU; box = box_rows x 64 columns, 128-byte swizzle, zeros outside.
 bool make_map(CUtensorMap* m, const void* base, uint64_t rows, uint64_t K, uint32_t box_rows) {
     EncodeTiledFn fn = encode_tiled_fn();

@@ -1,0 +1,619 @@
+// Attention of the rows of draft trees over a cache kept in pages (include/sdv.h: sdv_tree_attention).
+#pragma once
+#include <cuda.h>
+#include <math_constants.h>
+
+#include "paged.cuh"
+#include "tree_plan.h"
+
+namespace sdv {
+
+constexpr int kTreeThreads = 192;      // warps 0..3: softmax, a tile row per thread; 4: copies; 5: tensor-core issue
+constexpr int kTreeBlocksPerSm = 2;
+constexpr int kTreeMaxBlocks = 1024;   // of a launch: twice the SMs
+
+template <int HD>
+struct TreeShape {
+    static constexpr int kAtoms = HD / 64;                        // 64-column swizzled slabs of a row
+    static constexpr int kQBytes = kTreeTileRows * HD * 2;
+    static constexpr int kSlotBytes = kTreeKeys * HD * 2;         // keys or values of a tile
+    static constexpr int kSlots = HD == 128 ? 5 : 12;
+    static constexpr int kCtlBytes = 1024;
+    static constexpr int kSmemBytes = kQBytes + kSlots * kSlotBytes + kCtlBytes;   // two blocks an SM: at most 113 KB each
+    static_assert(kSmemBytes <= 113 * 1024, "two blocks per SM");
+};
+
+struct TreeParams : TreeLists {
+    const void* q;
+    void* out;
+    const void* v;                     // pool, for values that are not finite
+    const int *block_table, *parent;
+    long long* tiles_before;           // [n_seqs + 1] tiles of the sequences before, for the merge
+    float* part_o;                     // [block][2][part_rows][HD]
+    float2* part_ml;                   // [block][2][part_rows] maximum (log2 units), sum
+    int* status;
+    long long q_row_stride, q_head_stride, out_row_stride, out_head_stride, table_stride, page_stride, head_stride, token_stride;
+    int page_shift, n_pages, part_rows, blocks;
+    float scale_log2e;
+    unsigned long long wait_limit_ns;
+};
+
+__device__ __forceinline__ void tma_load_4d(void* smem_dst, const void* map, int x, int y, int z, int w, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(smem_u32(smem_dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+                 : "memory");
+}
+
+template <typename T> __device__ __forceinline__ uint32_t tree_idesc(uint32_t n);
+template <> __device__ __forceinline__ uint32_t tree_idesc<__nv_bfloat16>(uint32_t n) { return umma_idesc_bf16(128u, n); }
+template <> __device__ __forceinline__ uint32_t tree_idesc<__half>(uint32_t n) { return umma_idesc_bf16(128u, n) & ~((1u << 7) | (1u << 10)); }   // both operands fp16
+
+// Clears what is infinite or NaN among the two 16-bit numbers of a word; whether there was any.
+template <typename T> __device__ __forceinline__ bool clear_not_finite(uint32_t& w) {
+    constexpr uint32_t kExp = Half16<T>::kExponent;
+    const bool lo = (w & kExp) == kExp, hi = ((w >> 16) & kExp) == kExp;
+    w &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+    return lo || hi;
+}
+
+// Bit masks of the rows on the way from every row of a tree to its root, by doubling: lane l has rows l and l + 32.
+__device__ __forceinline__ void tree_masks(const TreeParams& P, const TreeSeq& s, int lane, unsigned long long& m0, unsigned long long& m1) {
+    int p0 = lane, p1 = lane + 32;   // how far up the mask reaches: a row points at itself once it is at the root
+    m0 = 1ull << lane;
+    m1 = 1ull << (lane + 32);
+    if (lane > 0 && lane < s.rows) {
+        const int p = __ldg(P.parent + s.first + lane);
+        p0 = p < 0 || p >= lane ? 0 : p;
+    }
+    if (lane + 32 < s.rows) {
+        const int p = __ldg(P.parent + s.first + lane + 32);
+        p1 = p < 0 || p >= lane + 32 ? 0 : p;
+    }
+    m0 |= 1ull << p0;
+    m1 |= 1ull << p1;
+#pragma unroll 1
+    for (int step = 0; step < 6 && __any_sync(0xffffffffu, p0 > 0 && p0 != lane || p1 > 0 && p1 != lane + 32); ++step) {
+        const unsigned long long a0 = __shfl_sync(0xffffffffu, m0, p0 & 31), a1 = __shfl_sync(0xffffffffu, m1, p0 & 31);
+        const unsigned long long b0 = __shfl_sync(0xffffffffu, m0, p1 & 31), b1 = __shfl_sync(0xffffffffu, m1, p1 & 31);
+        const int q0 = __shfl_sync(0xffffffffu, p0, p0 & 31), q1 = __shfl_sync(0xffffffffu, p1, p0 & 31);
+        const int r0 = __shfl_sync(0xffffffffu, p0, p1 & 31), r1 = __shfl_sync(0xffffffffu, p1, p1 & 31);
+        m0 |= p0 < 32 ? a0 : a1;
+        m1 |= p1 < 32 ? b0 : b1;
+        p0 = p0 < 32 ? q0 : q1;
+        p1 = p1 < 32 ? r0 : r1;
+    }
+}
+
+// Values of the rows `rows` of the tree that are not finite, columns c .. c + 31, added to a row's output: the product left them out.  An infinity times any
+// probability is the infinity, so no weight is needed.  Rare.
+template <typename T>
+__device__ __forceinline__ void tree_add_not_finite(const TreeParams& P, const TreeCursor& cur, unsigned long long rows, int c, uint32_t (&o)[32]) {
+#pragma unroll 1
+    for (; rows; rows &= rows - 1) {
+        const int key = cur.s.length + __ffsll((long long)rows) - 1;
+        const int page = __ldg(P.block_table + cur.b * P.table_stride + (key >> P.page_shift));
+        if (page < 0 || page >= P.n_pages) continue;
+        const T* v = (const T*)P.v + page * P.page_stride + cur.h * P.head_stride + (key & (P.page_size - 1)) * P.token_stride + c;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float x = Half16<T>::up(v[i]);
+            if (!isfinite(x)) o[i] = __float_as_uint(__uint_as_float(o[i]) + x);
+        }
+    }
+}
+
+// All tiles of 64 keys of all sequences, KV heads and chunks of 128 query rows (a tile row is one query head of one row; the heads that share a KV head
+// and the rows of a sequence read the keys together) are one list, cut into equal shares over two blocks per SM, whatever the lengths: a block works through
+// parts of one or of many items, and what it did not do alone is merged by tree_merge_kernel from un-normalised outputs, maxima and sums in the workspace.
+// Within a block: keys and values come page by page through a ring of tensor-map copies; S = Q K^T goes to one of two tensor-memory buffers, is turned into
+// probabilities in place (a row per thread, no exchange between threads) and P V adds up in tensor memory, where it is rescaled only when a row's maximum grew by
+// more than 2^8 (the published FlashAttention-4 rule: probabilities stay below 2^8, sums are fp32).  S of the next tile is computed during
+// the softmax of this one.  A step over a long cache is bound by memory: 128 rows cost 0.35 us of tensor work and 0.3 us of exponentials
+// per tile of 64 keys and SM where the copies take 0.75 us.
+// Places behind a sequence's end hold anything: their values are cleared in shared memory (0 x NaN is not 0).  Rows of the tree
+// that a row does not see take part in its product with probability 0: infinities and NaN among their values are cleared too, and added
+// by those who see them at the end.
+template <typename T, int HD>
+__global__ void __launch_bounds__(kTreeThreads, kTreeBlocksPerSm)
+tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TreeParams P) {
+    using S = TreeShape<HD>;
+    constexpr int KSTEPS = HD / 16, UNITS = HD / 8;
+    extern __shared__ __align__(1024) uint8_t tree_smem[];
+    uint8_t *Qs = tree_smem, *ring = Qs + S::kQBytes;
+    struct Ctl {
+        uint64_t full[S::kSlots], empty[S::kSlots], s_full[2], p_ready[2], pv_done[2], q_ready, drained;
+        unsigned long long bad[4];     // rows of the tree with values that are not finite, by item (modulo 4)
+        long long warp_sum[kTreeThreads / 32], total, offset;
+        uint32_t tmem_base;
+        int abort_flag, b0;
+    };
+    Ctl* ctl = reinterpret_cast<Ctl*>(ring + S::kSlots * S::kSlotBytes);
+    static_assert(sizeof(Ctl) <= S::kCtlBytes, "control block");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
+    if (tid == 0) {
+        for (int s = 0; s < S::kSlots; ++s) {
+            mbar_init(&ctl->full[s], 1);
+            mbar_init(&ctl->empty[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&ctl->s_full[i], 1);
+            mbar_init(&ctl->p_ready[i], 4);
+            mbar_init(&ctl->pv_done[i], 1);
+        }
+        for (int i = 0; i < 4; ++i) ctl->bad[i] = 0;
+        mbar_init(&ctl->drained, 1);
+        mbar_init(&ctl->q_ready, 4);
+        ctl->abort_flag = 0;
+        mbar_fence_init();
+    }
+    if (warp == 5) tmem_alloc(&ctl->tmem_base, 256);   // S0 | S1, 64 columns each | O, HD columns
+    // tiles of every sequence, summed up: each thread takes a run of sequences
+    const int B = P.n_seqs, per = (B + kTreeThreads - 1) / kTreeThreads, sb0 = min(tid * per, B), sb1 = min(sb0 + per, B);
+    long long sum = 0;
+    for (int b = sb0; b < sb1; ++b) sum += tree_tiles(P, tree_seq(P, b));
+    long long incl = sum;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += v;
+    }
+    if (lane == 31) ctl->warp_sum[warp] = incl;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctl->tmem_base;
+    grid_dep_launch();
+    long long before = incl - sum, total = 0;
+    for (int w = 0; w < kTreeThreads / 32; ++w) {
+        if (w < warp) before += ctl->warp_sum[w];
+        total += ctl->warp_sum[w];
+    }
+    const int sharers = tree_sharers(total, P.blocks);
+    const long long my0 = tree_share(total, (int)blockIdx.x, sharers), my1 = tree_share(total, (int)blockIdx.x + 1, sharers);
+    if (blockIdx.x == 0 || (my0 < my1 && my0 >= before && my0 < before + sum)) {
+        long long at = before;
+        for (int b = sb0; b < sb1; ++b) {
+            const long long n = tree_tiles(P, tree_seq(P, b));
+            if (blockIdx.x == 0) P.tiles_before[b] = at;
+            if (my0 >= at && my0 < at + n) {
+                ctl->b0 = b;
+                ctl->offset = my0 - at;
+            }
+            at += n;
+        }
+        if (blockIdx.x == 0 && tid == kTreeThreads - 1) P.tiles_before[B] = total;
+    }
+    __syncthreads();
+    TreeCursor cur;
+    cur.start(P, my0 < my1 ? ctl->b0 : 0, my0 < my1 ? ctl->offset : 0, my1 - my0);
+
+    if (warp == 4) {
+        // ---- copies: K0 V0 K1 V1 ... through the ring
+        const int box_keys = min(P.page_size, kTreeKeys), boxes = kTreeKeys / box_keys;   // per slab
+        const int my_box = lane % boxes, my_atom = lane / boxes;
+        uint32_t s = 0, par = 0;
+        long long issued = 0;
+        bool ok = true;
+        const auto page_of = [&](const TreeCursor& c, int tile) {   // page of this lane's box of a tile
+            const int key = tile * kTreeKeys + my_box * box_keys;
+            return my_atom < S::kAtoms && key < c.s.keys ? __ldg(P.block_table + c.b * P.table_stride + (key >> P.page_shift)) : -1;
+        };
+        int page = cur.left > 0 ? page_of(cur, cur.tile) : -1;
+        while (cur.left > 0 && ok) {
+            const int n = cur.run();
+            TreeCursor nxt = cur;
+            nxt.skip(P, n);
+            for (int j = 0; j < n && ok; ++j) {
+                const int tile = cur.tile + j, key = tile * kTreeKeys + my_box * box_keys;
+                const int next_page = j + 1 < n ? page_of(cur, tile + 1) : nxt.left > 0 ? page_of(nxt, nxt.tile) : -1;
+                const bool mine = my_atom < S::kAtoms && key < cur.s.keys;
+                const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)box_keys * 128u;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    ok = ok && mbar_wait_bounded(&ctl->empty[s], par ^ 1u, &ctl->abort_flag, P.wait_limit_ns);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx(&ctl->full[s], bytes);
+                    __syncwarp();
+                    // (x a multiple of 64 elements; a page outside the pool reads as zeros)
+                    if (mine)
+                        tma_load_4d(ring + s * S::kSlotBytes + my_atom * (kTreeKeys * 128) + my_box * box_keys * 128, kv ? &map_v : &map_k, my_atom * 64, key & (P.page_size - 1),
+                                    cur.h, page, &ctl->full[s]);
+                    ++issued;
+                    if (++s == S::kSlots) { s = 0; par ^= 1u; }
+                }
+                page = next_page;
+            }
+            cur = nxt;
+        }
+        // the copies still in flight are waited for (bounded): where a wait was given up, here or later, nobody else does
+        for (int back = 0; back < S::kSlots && back < issued; ++back) {
+            if (s == 0) { s = S::kSlots; par ^= 1u; }
+            --s;
+            if (!mbar_drain(&ctl->full[s], par, P.wait_limit_ns)) break;
+        }
+    } else if (warp == 5) {
+        // ---- tensor-core issue
+        const uint32_t id_s = tree_idesc<T>(kTreeKeys), id_o = tree_idesc<T>(HD) | (1u << 16);   // B of P V: features contiguous
+        const uint32_t qa = smem_u32(Qs), ra = smem_u32(ring);
+        bool ok = true;
+        uint32_t item = 0;
+        uint32_t s_k = 0, par_k = 0;                    // slot of the next keys
+        uint32_t n_s = 0, n_p = 0;                      // tiles whose scores / products were issued
+        const auto wait = [&](uint64_t* bar, uint32_t parity) {
+            ok = ok && mbar_wait_bounded(bar, parity, &ctl->abort_flag, P.wait_limit_ns);
+            ok = __all_sync(0xffffffffu, ok);
+        };
+        const auto scores = [&]() {
+            // the buffer held the probabilities of the tile two back: products into different accumulators are not ordered among themselves
+            // (waited for is the newest product: within an item that of the tile two back)
+            if (n_p > 0) wait(&ctl->pv_done[(n_p - 1u) & 1u], ((n_p - 1u) >> 1) & 1u);
+            wait(&ctl->full[s_k], par_k);
+            if (!ok) return;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t d = tmem + (n_s & 1u) * kTreeKeys, k = ra + s_k * S::kSlotBytes;
+#pragma unroll
+                for (int ks = 0; ks < KSTEPS; ++ks)
+                    umma_bf16(d, umma_desc_sw128(qa + (uint32_t)((ks >> 2) * (kTreeTileRows * 128) + (ks & 3) * 32)),
+                              umma_desc_sw128(k + (uint32_t)((ks >> 2) * (kTreeKeys * 128) + (ks & 3) * 32)), id_s, (uint32_t)ks);
+                umma_commit(&ctl->empty[s_k]);
+                umma_commit(&ctl->s_full[n_s & 1u]);
+            }
+            __syncwarp();
+            ++n_s;
+            s_k += 2;                                   // the values lie between
+            if (s_k >= S::kSlots) { s_k -= S::kSlots; par_k ^= 1u; }
+        };
+        uint32_t s_v = 1, par_v = 0;
+        while (cur.left > 0 && ok) {
+            const int n = cur.run();
+            wait(&ctl->q_ready, item & 1u);
+            if (ok) scores();
+            for (int j = 0; j < n && ok; ++j) {
+                if (j + 1 < n) scores();
+                wait(&ctl->full[s_v], par_v);
+                wait(&ctl->p_ready[n_p & 1u], (n_p >> 1) & 1u);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t p = tmem + (n_p & 1u) * kTreeKeys, v = ra + s_v * S::kSlotBytes;
+#pragma unroll
+                    for (int ks = 0; ks < kTreeKeys / 16; ++ks)   // 16 keys: 16 rows of 128 bytes of every slab; 8 packed columns of P
+                        umma_bf16_tmem_a(tmem + 2 * kTreeKeys, p + (uint32_t)ks * 8u, umma_desc_sw128_mn(v + (uint32_t)ks * 2048u, kTreeKeys * 128), id_o,
+                                         (uint32_t)(j | ks));
+                    umma_commit(&ctl->empty[s_v]);
+                    umma_commit(&ctl->pv_done[n_p & 1u]);
+                }
+                __syncwarp();
+                ++n_p;
+                s_v += 2;
+                if (s_v >= S::kSlots) { s_v -= S::kSlots; par_v ^= 1u; }
+            }
+            ++item;
+            cur.skip(P, n);
+        }
+        if (!ok) {
+            // behind an abandoned wait: tensor and shared memory are given back only when no product uses them any more
+            if (elect_one()) umma_commit(&ctl->drained);
+            __syncwarp();
+            mbar_drain(&ctl->drained, 0, P.wait_limit_ns);
+        }
+    } else {
+        // ---- softmax: tile row t
+        const int t = tid;
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16, to = tmem + lanes + 2 * kTreeKeys;
+        bool ok = true;
+        uint32_t n_t = 0, item = 0;
+        int mask_b = -1;
+        unsigned long long anc0 = 0, anc1 = 0;
+        uint32_t v_slot = 1, v_par = 0;
+        const auto load_q = [&](const TreeCursor& c) {   // the item's query rows; tile rows without one keep what they hold
+            const int r = c.c * kTreeTileRows + t, j = r / P.g, hh = r - j * P.g;
+            if (j < c.s.rows) {
+                const uint4* src = reinterpret_cast<const uint4*>((const T*)P.q + (c.s.first + j) * P.q_row_stride + (c.h * P.g + hh) * P.q_head_stride);
+                uint4 v[UNITS];
+#pragma unroll
+                for (int i = 0; i < UNITS; ++i) v[i] = __ldg(src + i);
+#pragma unroll
+                for (int i = 0; i < UNITS; ++i) *reinterpret_cast<uint4*>(Qs + (i >> 3) * (kTreeTileRows * 128) + swz_unit(t, i & 7)) = v[i];
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl->q_ready);
+        };
+        if (cur.left > 0) load_q(cur);
+        while (cur.left > 0) {
+            const int n = cur.run();
+            const TreeSeq& sq = cur.s;
+            const int r = cur.c * kTreeTileRows + t, j = r / P.g, hh = r - j * P.g;
+            const bool real = j < sq.rows, some = cur.c * kTreeTileRows + warp * 32 < sq.rows * P.g;   // this row, any row of the warp
+            unsigned long long see = j < 63 ? (2ull << j) - 1 : ~0ull;                                 // rows of the sequence this row sees
+            if (P.parent) {
+                if (mask_b != cur.b) {
+                    tree_masks(P, sq, lane, anc0, anc1);
+                    mask_b = cur.b;
+                }
+                const unsigned long long a0 = __shfl_sync(0xffffffffu, anc0, j & 31), a1 = __shfl_sync(0xffffffffu, anc1, j & 31);
+                see = j < 32 ? a0 : a1;
+            }
+            float m = -CUDART_INF_F, l = 0.f;
+            for (int k = 0; k < n; ++k, ++n_t) {
+                const int key0 = (cur.tile + k) * kTreeKeys, new0 = sq.length - key0, left = sq.keys - key0;   // first new key, keys left, within the tile
+                const uint32_t ts = tmem + lanes + (n_t & 1u) * kTreeKeys;
+                ok = ok && mbar_wait_bounded(&ctl->s_full[n_t & 1u], (n_t >> 1) & 1u, &ctl->abort_flag, P.wait_limit_ns);
+                const bool tail = new0 < kTreeKeys;    // rows of the tree, or the end, among the keys
+                if (tail) {
+                    ok = ok && mbar_wait_bounded(&ctl->full[v_slot], v_par, &ctl->abort_flag, P.wait_limit_ns);
+                    if (ok) {
+                        // two threads a key, half of its columns each
+                        const int key = t >> 1;
+                        uint4* vr = reinterpret_cast<uint4*>(ring + v_slot * S::kSlotBytes + key * 128);
+                        bool wrong = false;
+#pragma unroll
+                        for (int i = (t & 1) * 4; i < (t & 1) * 4 + 4; ++i) {
+#pragma unroll
+                            for (int a = 0; a < S::kAtoms; ++a) {
+                                uint4* w = vr + a * (kTreeKeys * 8) + i;
+                                if (key >= left) *w = make_uint4(0, 0, 0, 0);
+                                else if (key >= new0) {
+                                    uint4 x = *w;
+                                    if (clear_not_finite<T>(x.x) | clear_not_finite<T>(x.y) | clear_not_finite<T>(x.z) | clear_not_finite<T>(x.w)) {
+                                        *w = x;
+                                        wrong = true;
+                                    }
+                                }
+                            }
+                        }
+                        if (wrong) atomicOr(&ctl->bad[item & 3u], 1ull << (key - new0));
+                    }
+                    fence_proxy_async_smem();
+                }
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (some) {
+                    tc_fence_after();
+                    uint32_t v[2][32];
+                    tmem_ld32(ts, v[0]);
+                    tmem_ld32(ts + 32u, v[1]);
+                    tmem_ld_wait();
+                    if (tail) {
+                        // keys before the new ones, and the new ones on the row's path
+                        const int old = max(new0, 0);
+                        unsigned long long vis = old >= 64 ? ~0ull : (1ull << old) - 1;
+                        if (new0 >= 0) vis |= new0 < 64 ? see << new0 : 0ull;
+                        else vis |= -new0 < 64 ? see >> -new0 : 0ull;
+                        if (left < 64) vis &= (1ull << left) - 1;
+#pragma unroll
+                        for (int i = 0; i < 64; ++i)
+                            if (!((vis >> i) & 1ull)) v[i >> 5][i & 31] = 0xff800000u;   // -inf
+                    }
+                    float m4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(v[i >> 5][i & 31]));
+                    const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * P.scale_log2e;
+                    const bool grow = real && mx > m + 8.f;   // also the first tile that shows this row a key
+                    const bool rescale = grow && m != -CUDART_INF_F;
+                    if (__any_sync(0xffffffffu, rescale)) {
+                        // the product of the tile before has to be complete (it is the newest one, as this tile's waits for this
+                        // warp, and the one two before it is complete, as these scores came after it: with two barriers the parity is unambiguous)
+                        ok = mbar_wait_bounded(&ctl->pv_done[(n_t - 1u) & 1u], ((n_t - 1u) >> 1) & 1u, &ctl->abort_flag, P.wait_limit_ns);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const float f = rescale ? exp2f(m - mx) : 1.f;
+                        l *= f;
+#pragma unroll 1
+                        for (int c = 0; c < HD; c += 16) {
+                            float o[16];
+                            uint32_t x[16];
+                            tmem_ld16(to + (uint32_t)c, o);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(o[i] * f);
+                            tmem_st16(to + (uint32_t)c, x);
+                        }
+                    }
+                    if (grow) m = mx;
+                    const float ref = m == -CUDART_INF_F ? 0.f : m;
+                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            const float x = ex2_ftz(fmaf(__uint_as_float(v[c][i]), P.scale_log2e, -ref));
+                            const float y = ex2_ftz(fmaf(__uint_as_float(v[c][i + 1]), P.scale_log2e, -ref));
+                            s4[i & 2] += x;
+                            s4[(i & 2) + 1] += y;
+                            pk[i / 2] = Half16<T>::pack(x, y);
+                        }
+                        tmem_st16(ts + 16u * (uint32_t)c, pk);   // over scores this thread has read
+                    }
+                    l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    tmem_st_wait();
+                    tc_fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl->p_ready[n_t & 1u]);
+                v_slot += 2;
+                if (v_slot >= S::kSlots) { v_slot -= S::kSlots; v_par ^= 1u; }
+            }
+            // The scores of the item's last tile were read by every warp before it announced its probabilities, but a slower warp's queries may still be
+            // in use: they are not, once the scores are there (s_full of the last tile).  The next item's queries go in while P V finishes.
+            TreeCursor nxt = cur;
+            nxt.skip(P, n);
+            if (nxt.left > 0 && ok) load_q(nxt);
+            if (ok) ok = mbar_wait_bounded(&ctl->pv_done[(n_t - 1u) & 1u], ((n_t - 1u) >> 1) & 1u, &ctl->abort_flag, P.wait_limit_ns);
+            ok = __all_sync(0xffffffffu, ok);
+            const bool whole = n == sq.tiles;
+            if (some) {
+                tc_fence_after();
+                const unsigned long long bad = *(volatile unsigned long long*)&ctl->bad[item & 3u] & see;
+                const int slot = (int)blockIdx.x * 2 + (item ? 1 : 0);   // an item that is not the block's first is its last, or whole
+                float* po = P.part_o + ((long long)slot * P.part_rows + t) * HD;
+                T* dst = (T*)P.out + (sq.first + j) * P.out_row_stride + (cur.h * P.g + hh) * P.out_head_stride;
+                const float sc = whole ? 1.f / l : 1.f;
+                if (!whole && real) P.part_ml[(long long)slot * P.part_rows + t] = ok ? make_float2(m, l) : make_float2(0.f, CUDART_NAN_F);
+#pragma unroll 1
+                for (int c = 0; c < HD; c += 32) {
+                    uint32_t o[32];
+                    if (ok) {
+                        tmem_ld32(to + (uint32_t)c, o);
+                        tmem_ld_wait();
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = 0x7fc00000u;   // NaN
+                    }
+                    if (real && ok && bad) tree_add_not_finite<T>(P, cur, bad, c, o);
+                    if (!real) continue;
+                    if (whole) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8)
+                            *reinterpret_cast<uint4*>(dst + c + i) =
+                                make_uint4(Half16<T>::pack(__uint_as_float(o[i]) * sc, __uint_as_float(o[i + 1]) * sc), Half16<T>::pack(__uint_as_float(o[i + 2]) * sc, __uint_as_float(o[i + 3]) * sc),
+                                           Half16<T>::pack(__uint_as_float(o[i + 4]) * sc, __uint_as_float(o[i + 5]) * sc), Half16<T>::pack(__uint_as_float(o[i + 6]) * sc, __uint_as_float(o[i + 7]) * sc));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) st_global_v8(po + c + i, o + i);
+                    }
+                }
+                tc_fence_before();
+            }
+            // nobody is at the item after the next before this thread has been through the next one, and all are done with the one two back
+            if (tid == 0) ctl->bad[(item + 2u) & 3u] = 0;
+            ++item;
+            cur = nxt;
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (warp == 5) tmem_dealloc(tmem, 256);
+    if (tid == 0 && ctl->abort_flag && P.status) atomicExch(P.status, 1);
+}
+
+// Output rows whose keys several blocks went through: un-normalised partial outputs weighted by 2^(maximum - largest maximum).  A block takes `group` pairs of row and
+// query head at a time; a pair with up to eight parts is one warp's, one with more the whole block's (a long cache of few sequences is cut into up to 150
+// parts: read by one warp, they would take longer than the attention).
+constexpr int kMergeThreads = 256, kMergeWarps = kMergeThreads / 32;
+struct TreePart {   // where the parts of an output row are
+    int block0, n, row;   // first block, blocks, tile row
+    bool late;            // of block0 it is the second partial item
+    __device__ __forceinline__ long long at(const TreeParams& P, int i) const { return ((long long)(block0 + i) * 2 + (i == 0 && late ? 1 : 0)) * P.part_rows + row; }
+};
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_constant__ TreeParams P, int group) {
+    constexpr int VEC = HD / 32;   // columns of a lane
+    __shared__ TreePart shared_part[kMergeWarps];
+    __shared__ float weight[kTreeMaxBlocks], red[kMergeWarps], sums[kMergeWarps][HD];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_q = P.n_kv * P.g, B = P.n_seqs;
+    const long long pairs = (long long)P.n_rows * n_q;
+    grid_dep_wait();
+    const long long total = P.tiles_before[B];
+    const auto store = [&](long long pair, const float (&o)[VEC], float sum) {
+        const int r = (int)(pair / n_q), hq = (int)(pair - (long long)r * n_q);
+        T* dst = (T*)P.out + r * P.out_row_stride + hq * P.out_head_stride + lane * VEC;
+        const float sc = 1.f / sum;
+        if constexpr (VEC == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(Half16<T>::pack(o[0] * sc, o[1] * sc), Half16<T>::pack(o[2] * sc, o[3] * sc));
+        else *reinterpret_cast<uint32_t*>(dst) = Half16<T>::pack(o[0] * sc, o[1] * sc);
+    };
+    const auto add = [&](float (&o)[VEC], float w, long long at) {
+        const float* src = P.part_o + at * HD + lane * VEC;
+        if constexpr (VEC == 4) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
+            o[0] += w * x.x; o[1] += w * x.y; o[2] += w * x.z; o[3] += w * x.w;
+        } else {
+            const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
+            o[0] += w * x.x; o[1] += w * x.y;
+        }
+    };
+    for (long long p0 = (long long)blockIdx.x * group; p0 < pairs; p0 += (long long)gridDim.x * group) {
+        TreePart part;
+        part.n = 0;
+        const long long pair = p0 + warp;
+        if (warp < group && pair < pairs && total > 0) {
+            const int r = (int)(pair / n_q), hq = (int)(pair - (long long)r * n_q);
+            // the row's sequence: the last one that begins at or before it, by two (for over 1024 sequences more) ballots
+            int lo = 0, n = B;   // among lo .. lo + n - 1
+            while (n > 1) {
+                const int step = (n + 31) / 32, at = lo + lane * step;
+                const bool begins = lane * step < n && rows_begin(P.cu_rows, at, P.n_rows) <= r;
+                const int k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, begins)));
+                n = min(step, n - k * step);
+                lo += k * step;
+            }
+            const TreeSeq s = tree_seq(P, lo);
+            const int j = r - s.first;
+            if (j >= 0 && j < s.rows && s.tiles > 0) {
+                const int h = hq / P.g, tr = j * P.g + hq - h * P.g, c = tr / kTreeTileRows;
+                const long long tile0 = P.tiles_before[lo] + ((long long)h * s.chunks + c) * s.tiles;
+                const int sharers = tree_sharers(total, P.blocks);
+                part.block0 = tree_owner(total, tile0, sharers);
+                part.n = tree_owner(total, tile0 + s.tiles - 1, sharers) - part.block0 + 1;
+                part.row = tr - c * kTreeTileRows;
+                part.late = tree_share(total, part.block0, sharers) < tile0;
+            }
+        }
+        if (part.n > 1 && part.n <= 8) {
+            const float2 ml = lane < part.n ? __ldcg(P.part_ml + part.at(P, lane)) : make_float2(-CUDART_INF_F, 0.f);
+            float mx = ml.x;
+#pragma unroll
+            for (int off = 4; off; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+            mx = __shfl_sync(0xffffffffu, mx, 0);
+            const float w = exp2f(ml.x - (mx == -CUDART_INF_F ? 0.f : mx));
+            float sum = w * ml.y;
+#pragma unroll
+            for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            float o[VEC] = {};
+            for (int i = 0; i < part.n; ++i) add(o, __shfl_sync(0xffffffffu, w, i), part.at(P, i));
+            store(pair, o, sum);
+        }
+        if (lane == 0) shared_part[warp] = part;
+        __syncthreads();
+        for (int k = 0; k < group; ++k) {
+            const TreePart q = shared_part[k];
+            if (q.n <= 8) continue;   // the same for the whole block
+            float mx = -CUDART_INF_F;
+            for (int i = threadIdx.x; i < q.n; i += kMergeThreads) mx = fmaxf(mx, __ldcg(P.part_ml + q.at(P, i)).x);
+#pragma unroll
+            for (int off = 16; off; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+            if (lane == 0) red[warp] = mx;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kMergeWarps; ++w) mx = fmaxf(mx, red[w]);
+            const float ref = mx == -CUDART_INF_F ? 0.f : mx;
+            float sum = 0.f;
+            for (int i = threadIdx.x; i < q.n; i += kMergeThreads) {
+                const float2 ml = __ldcg(P.part_ml + q.at(P, i));
+                weight[i] = exp2f(ml.x - ref);
+                sum += weight[i] * ml.y;
+            }
+#pragma unroll
+            for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            __syncthreads();   // the maxima have been read
+            if (lane == 0) red[warp] = sum;
+            __syncthreads();
+            sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kMergeWarps; ++w) sum += red[w];
+            float o[VEC] = {};
+#pragma unroll 8
+            for (int i = warp; i < q.n; i += kMergeWarps) add(o, weight[i], q.at(P, i));
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) sums[warp][lane * VEC + v] = o[v];
+            __syncthreads();
+            if (warp == 0) {
+                float t[VEC] = {};
+#pragma unroll
+                for (int w = 0; w < kMergeWarps; ++w)
+#pragma unroll
+                    for (int v = 0; v < VEC; ++v) t[v] += sums[w][lane * VEC + v];
+                store(p0 + k, t, sum);
+            }
+            __syncthreads();
+        }
+        __syncthreads();   // shared_part is read before the next pairs'
+    }
+}
+
+}  // namespace sdv

@@ -1,0 +1,91 @@
+// How the attention over pages cuts its work: sequences, tiles, shares of blocks.  Host and device code.
+#pragma once
+#include <stdint.h>
+
+#include "../../include/sdv.h"
+
+#ifdef __CUDACC__
+#define SDV_HD __host__ __device__ __forceinline__
+#else
+#define SDV_HD inline
+#endif
+#ifdef __CUDA_ARCH__
+#define SDV_LD(p) __ldg(p)
+#else
+#define SDV_LD(p) (*(p))
+#endif
+
+namespace sdv {
+
+#ifndef __CUDACC__
+template <typename T> inline T min(T a, T b) { return b < a ? b : a; }
+template <typename T> inline T max(T a, T b) { return a < b ? b : a; }
+#endif
+
+constexpr int kTreeKeys = 64;          // keys of a tile
+constexpr int kTreeTileRows = 128;     // query rows of a tile: one query head of one row each
+
+// The caller's index arrays and sizes.
+struct TreeLists {
+    const int *kv_len, *cu_rows;
+    int n_seqs, n_rows, n_kv, g, table_width, page_size;   // g: query heads per KV head
+};
+
+// Rows of sequence b, whatever cu_rows holds: within [0, n_rows), none where the array descends.
+SDV_HD int rows_begin(const int* cu, int b, int n_rows) { return min(max(SDV_LD(cu + b), 0), n_rows); }
+SDV_HD int rows_count(const int* cu, int b, int n_rows) { return max(0, rows_begin(cu, b + 1, n_rows) - rows_begin(cu, b, n_rows)); }
+
+// One sequence as the kernels see it, whatever the arrays hold.
+struct TreeSeq {
+    int first, rows, length, keys;     // first row, rows, committed tokens, tokens in all (those the block table has room for)
+    int chunks, tiles;                 // tiles of 128 query rows (row, head of the group), tiles of keys
+};
+SDV_HD TreeSeq tree_seq(const TreeLists& P, int b) {
+    TreeSeq s;
+    s.first = rows_begin(P.cu_rows, b, P.n_rows);
+    s.rows = min(rows_count(P.cu_rows, b, P.n_rows), SDV_TREE_ROWS);
+    const long long room = min((long long)P.table_width * P.page_size, 0x7fffffffll - kTreeKeys);
+    s.length = (int)min((long long)max(SDV_LD(P.kv_len + b), 0), room);
+    s.keys = (int)min((long long)s.length + s.rows, room);
+    s.chunks = (s.rows * P.g + kTreeTileRows - 1) / kTreeTileRows;
+    s.tiles = s.rows ? (s.keys + kTreeKeys - 1) / kTreeKeys : 0;
+    return s;
+}
+SDV_HD long long tree_tiles(const TreeLists& P, const TreeSeq& s) { return (long long)s.tiles * s.chunks * P.n_kv; }
+
+// The tiles of all sequences, KV heads and row chunks in a row are cut into equal shares, one a block.
+SDV_HD int tree_sharers(long long total, int blocks) { return (int)min(total, (long long)blocks); }   // with one tile at least
+SDV_HD long long tree_share(long long total, int block, int sharers) { return block >= sharers ? total : total * block / sharers; }
+SDV_HD int tree_owner(long long total, long long tile, int sharers) { return (int)(((tile + 1) * sharers - 1) / total); }
+
+// Cursor over a block's tiles: sequence, KV head, row chunk, key tile.
+struct TreeCursor {
+    long long left;                    // tiles of the block still to do, this one included
+    int b, h, c, tile;
+    TreeSeq s;
+    SDV_HD void start(const TreeLists& P, int b0, long long offset, long long n) {
+        left = n;
+        b = b0;
+        if (n <= 0) return;
+        s = tree_seq(P, b);
+        tile = (int)(offset % s.tiles);
+        const long long item = offset / s.tiles;
+        c = (int)(item % s.chunks);
+        h = (int)(item / s.chunks);
+    }
+    // Tiles of the present item that belong to this block, from the present one on.
+    SDV_HD int run() const { return (int)min(left, (long long)(s.tiles - tile)); }
+    SDV_HD void skip(const TreeLists& P, int n) {   // n = run()
+        left -= n;
+        if (left <= 0) return;
+        tile = 0;
+        if (++c < s.chunks) return;
+        c = 0;
+        if (++h < P.n_kv) return;
+        h = 0;
+        do s = tree_seq(P, ++b); while (s.tiles == 0 && b + 1 < P.n_seqs);
+        if (s.tiles == 0) left = 0;
+    }
+};
+
+}  // namespace sdv

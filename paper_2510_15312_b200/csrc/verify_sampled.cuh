@@ -1,0 +1,299 @@
+// Verification of drafted tokens against the target's probabilities (include/sdv.h: sdv_verify_sampled).
+#pragma once
+#include "paged.cuh"
+
+namespace sdv {
+
+constexpr int kVerifyThreads = 512, kVerifyWarps = kVerifyThreads / 32;
+constexpr int kVerifyTile = 512;             // vocabulary entries a warp sums up at a time: four groups of four a lane
+constexpr int kVerifyMaxCluster = 8;
+
+__device__ __forceinline__ double ld_cluster_f8(uint32_t addr) {
+    double v;
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr));
+    return v;
+}
+
+// What the drawn token's distribution is made of.
+struct VerifyRest {
+    const float *p, *q;      // target's row; rejected draft's row or null
+    const int* out;          // tokens without a share (shared memory)
+    int n_out, vocab;
+    bool wide_p, wide_q;     // rows start on 16-byte boundaries
+};
+
+// Weights of entries at .. at + 3 (0 past the end) in 64 bits: the difference of two fp32 numbers is exact there.
+__device__ __forceinline__ void verify_weights(const VerifyRest& d, int at, double (&w)[4]) {
+    float p[4] = {0.f, 0.f, 0.f, 0.f}, q[4] = {0.f, 0.f, 0.f, 0.f};
+    if (at + 3 < d.vocab && d.wide_p) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(d.p + at));
+        p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (at + j < d.vocab) p[j] = __ldcg(d.p + at + j);
+    }
+    if (d.q) {
+        if (at + 3 < d.vocab && d.wide_q) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(d.q + at));
+            q[0] = v.x; q[1] = v.y; q[2] = v.z; q[3] = v.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (at + j < d.vocab) q[j] = __ldcg(d.q + at + j);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const double x = (double)p[j] - (double)q[j];
+        w[j] = p[j] > 0.f && x > 0.0 ? x : 0.0;   // NaN has no share either
+    }
+    for (int i = 0; i < d.n_out; ++i) {
+        const unsigned j = (unsigned)(d.out[i] - at);
+        if (j < 4u) {
+            if (j == 0) w[0] = 0.0;
+            if (j == 1) w[1] = 0.0;
+            if (j == 2) w[2] = 0.0;
+            if (j == 3) w[3] = 0.0;
+        }
+    }
+}
+
+// A cluster takes one sequence.  All its blocks go through the drafts (at most 64 rows, one gather each), each sums up its share of the distribution that
+// remains, tile by tile in a fixed order; the blocks' sums meet through distributed shared memory, and the block whose share holds the drawn token reads that one
+// tile again.  Sums in 64 bits: a token's share may be 10^-9 of the whole, fp32 sums would draw its neighbour.  Bound by reading the row (and
+// the draft's) once, for few sequences by the chain of round trips: rows, tokens, shares, row, tile.
+__global__ void __launch_bounds__(kVerifyThreads) verify_sampled_kernel(const __grid_constant__ sdv_verify_args a, int tiles_per_block) {
+    extern __shared__ double tile_sum[];   // [tiles_per_block]
+    __shared__ int tok[SDV_TREE_ROWS], par[SDV_TREE_ROWS], out[SDV_TREE_ROWS], path[SDV_TREE_ROWS], child[SDV_TREE_ROWS];
+    __shared__ float share[SDV_TREE_ROWS];
+    __shared__ unsigned char again[SDV_TREE_ROWS];
+    __shared__ int n_path, n_out, rejected_row;
+    __shared__ double total;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int CS = (int)cluster_size(), rank = (int)cluster_rank(), b = (int)blockIdx.x / CS;
+    const int first = rows_begin(a.cu_rows, b, a.n_rows), all = rows_count(a.cu_rows, b, a.n_rows), T = min(all, SDV_TREE_ROWS);
+    if (blockIdx.x == 0) {   // rows of no sequence
+        const int from = rows_begin(a.cu_rows, a.n_seqs, a.n_rows), until = rows_begin(a.cu_rows, 0, a.n_rows);
+        for (int r = tid; r < a.n_rows; r += kVerifyThreads) {
+            if (r >= until && r < from) continue;
+            a.out_tokens[r] = a.out_rows[r] = -1;
+            if (a.out_slots) a.out_slots[r] = -1;
+        }
+    }
+    if (T == 0) {   // the whole cluster
+        if (rank == 0 && tid == 0) a.accept_len[b] = -1;
+        return;
+    }
+    const int i = tid;
+    float u = 0.f, q = 1.f;
+    if (i < SDV_TREE_ROWS) {
+        int p = -1, x = -1;
+        float s = 0.f;
+        if (i > 0 && i < T) {
+            p = a.parent ? __ldg(a.parent + first + i) : i - 1;
+            if (p < 0 || p >= i) p = 0;
+            x = __ldg(a.tokens + first + i);
+            u = __ldg(a.uniforms + first + i);
+            if (x >= 0 && x < a.vocab) {
+                s = __ldcg(a.target + (first + p) * a.target_stride + x);
+                if (a.draft) q = __ldcg(a.draft + (first + i) * a.draft_stride + x);
+            }
+        }
+        tok[i] = x;
+        par[i] = p;
+        share[i] = s > 0.f ? s : 0.f;
+        child[i] = SDV_TREE_ROWS;
+    }
+    __syncthreads();
+    // siblings: whether an earlier one carries the same token, then what the earlier ones leave
+    if (i < T) {
+        bool same = false;
+        if (a.parent)
+            for (int s = 1; s < i; ++s) same |= par[s] == par[i] && tok[s] == tok[i];
+        again[i] = same;
+    }
+    __syncthreads();
+    if (i < T) {
+        bool yes = false;
+        if (i > 0) {
+            if (a.draft) {
+                yes = (double)u * (double)q < (double)share[i];
+            } else {
+                double gone = 0.0;
+                if (a.parent)
+                    for (int s = 1; s < i; ++s)
+                        if (par[s] == par[i] && !again[s]) gone += (double)share[s];
+                yes = !again[i] && (double)u * (1.0 - gone) < (double)share[i];
+            }
+        }
+        if (yes) atomicMin(&child[par[i]], i);   // the first accepted child is followed
+    }
+    __syncthreads();
+    if (tid == 0) {
+        int n = 0, at = 0;
+        path[0] = 0;
+        while (child[at] < SDV_TREE_ROWS) {
+            at = child[at];
+            path[++n] = at;
+        }
+        n_path = n;
+        n_out = 0;
+        rejected_row = -1;
+    }
+    __syncthreads();
+    const int a_len = n_path, last = path[a_len];
+    if (i > 0 && i < T && par[i] == last) {   // a rejected child: every child of the last accepted row is one
+        if (a.draft) rejected_row = i;
+        else out[atomicAdd(&n_out, 1)] = tok[i];   // any order: a set
+    }
+    if (rank == 0) {
+        // rows from the sequence's first on; the entry of the drawn token is written last, by whoever finds it
+        for (int r = tid; r < all; r += kVerifyThreads) {
+            a.out_rows[first + r] = r <= a_len ? path[min(r, SDV_TREE_ROWS - 1)] : -1;
+            if (r != a_len) a.out_tokens[first + r] = r < a_len ? tok[path[min(r + 1, SDV_TREE_ROWS - 1)]] : -1;
+        }
+        if (a.out_slots) {
+            for (int r = tid; r < all; r += kVerifyThreads) {
+                int to = -1;
+                for (int k = 1; k <= a_len; ++k)
+                    if (path[k] == r && k != r) to = __ldg(a.slots + first + k);
+                a.out_slots[first + r] = to;
+            }
+        }
+        if (tid == 0) a.accept_len[b] = a_len;
+    }
+    __syncthreads();
+    VerifyRest d;
+    d.vocab = a.vocab;
+    d.p = a.target + (first + last) * a.target_stride;
+    d.q = rejected_row >= 0 ? a.draft + (first + rejected_row) * a.draft_stride : nullptr;
+    d.out = out;
+    d.n_out = n_out;
+    d.wide_p = ((uintptr_t)d.p & 15) == 0;
+    d.wide_q = ((uintptr_t)d.q & 15) == 0;
+    const int tiles = (a.vocab + kVerifyTile - 1) / kVerifyTile, tile0 = rank * tiles_per_block, mine = max(0, min(tiles - tile0, tiles_per_block));
+    const float draw = __ldg(a.uniforms + first);
+    for (int attempt = 0;; ++attempt) {
+        for (int t = warp; t < mine; t += kVerifyWarps) {
+            double sum = 0.0;
+#pragma unroll
+            for (int k = 0; k < kVerifyTile / 128; ++k) {
+                double w[4];
+                verify_weights(d, (tile0 + t) * kVerifyTile + k * 128 + lane * 4, w);
+                sum += (w[0] + w[1]) + (w[2] + w[3]);
+            }
+#pragma unroll
+            for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            if (lane == 0) tile_sum[t] = sum;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            double sum = 0.0;
+            for (int t = lane; t < mine; t += 32) sum += tile_sum[t];
+#pragma unroll
+            for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            if (lane == 0) total = sum;
+            __syncwarp();
+        }
+        __syncthreads();
+        cluster_sync();
+        double before = 0.0, whole = 0.0;
+        int holder = -1;   // the first block behind which the cumulative sum exceeds the target, else the last one with a share
+        {
+            double sums[kVerifyMaxCluster];
+#pragma unroll
+            for (int k = 0; k < kVerifyMaxCluster; ++k) sums[k] = k < CS ? ld_cluster_f8(map_shared_rank(smem_u32(&total), k)) : 0.0;
+#pragma unroll
+            for (int k = 0; k < kVerifyMaxCluster; ++k) whole += sums[k];
+            const double goal = (double)draw * whole;
+            double cum = 0.0;
+            bool done = false;
+#pragma unroll
+            for (int k = 0; k < kVerifyMaxCluster; ++k) {
+                if (!done && sums[k] > 0.0) {
+                    holder = k;
+                    before = cum;
+                    done = cum + sums[k] > goal;
+                }
+                cum += sums[k];
+            }
+        }
+        cluster_sync();   // everybody has read the sums: they may be overwritten, and blocks may leave
+        if (!(whole > 0.0)) {
+            if (attempt == 0 && (d.q || d.n_out)) {   // nothing is left: the target's distribution itself
+                d.q = nullptr;
+                d.n_out = 0;
+                continue;
+            }
+            if (rank == 0 && tid == 0) a.out_tokens[first + a_len] = -1;
+            return;
+        }
+        if (rank != holder) return;
+        const double goal = (double)draw * whole;
+        if (warp == 0) {
+            // tile: the same rule over this block's tiles
+            double cum = before, at_before = before;
+            int at = -1;
+            bool done = false;
+            for (int t0 = 0; t0 < mine && !done; t0 += 32) {
+                const double x = t0 + lane < mine ? tile_sum[t0 + lane] : 0.0;
+                double incl = x;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const double v = __shfl_up_sync(0xffffffffu, incl, off);
+                    if (lane >= off) incl += v;
+                }
+                const unsigned some = __ballot_sync(0xffffffffu, x > 0.0), over = __ballot_sync(0xffffffffu, x > 0.0 && cum + incl > goal);
+                if (some) {
+                    const int l = over ? __ffs(over) - 1 : 31 - __clz(some);
+                    at = t0 + l;
+                    at_before = cum + __shfl_sync(0xffffffffu, incl - x, l);
+                    done = over != 0;
+                }
+                cum += __shfl_sync(0xffffffffu, incl, 31);
+            }
+            // entry: again over the tile's, in order
+            int token = -1;
+            cum = at_before;
+            done = false;
+            double w[kVerifyTile / 128][4];
+#pragma unroll
+            for (int k = 0; k < kVerifyTile / 128; ++k) verify_weights(d, (tile0 + at) * kVerifyTile + k * 128 + lane * 4, w[k]);
+#pragma unroll
+            for (int k = 0; k < kVerifyTile / 128; ++k) {
+                if (done) continue;
+                double part[4];
+                part[0] = w[k][0];
+                part[1] = part[0] + w[k][1];
+                part[2] = part[1] + w[k][2];
+                part[3] = part[2] + w[k][3];
+                double incl = part[3];
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const double v = __shfl_up_sync(0xffffffffu, incl, off);
+                    if (lane >= off) incl += v;
+                }
+                const double lead = cum + (incl - part[3]);
+                int hit = -1, some = -1;
+#pragma unroll
+                for (int j = 3; j >= 0; --j) {
+                    if (w[k][j] > 0.0 && lead + part[j] > goal) hit = j;
+                    if (w[k][3 - j] > 0.0) some = 3 - j;
+                }
+                const unsigned has = __ballot_sync(0xffffffffu, some >= 0), over = __ballot_sync(0xffffffffu, hit >= 0);
+                if (has) {
+                    const int l = over ? __ffs(over) - 1 : 31 - __clz(has);
+                    const int j = __shfl_sync(0xffffffffu, over ? hit : some, l);
+                    token = (tile0 + at) * kVerifyTile + k * 128 + l * 4 + j;
+                    done = over != 0;
+                }
+                cum += __shfl_sync(0xffffffffu, incl, 31);
+            }
+            if (lane == 0) a.out_tokens[first + a_len] = token;
+        }
+        return;
+    }
+}
+
+}  // namespace sdv
