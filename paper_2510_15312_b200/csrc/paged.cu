@@ -87,7 +87,7 @@ RopeKernel rope_kernel(int dtype, bool interleaved, int w) {
 }
 
 typedef void (*TreeKernel)(const CUtensorMap, const CUtensorMap, const TreeParams);
-typedef void (*MergeKernel)(const TreeParams, int);
+typedef void (*MergeKernel)(const TreeParams, int, int);
 TreeKernel tree_kernel(int dtype, int hd) {
     if (dtype == SDV_BF16) return hd == 128 ? tree_attention_kernel<__nv_bfloat16, 128> : tree_attention_kernel<__nv_bfloat16, 64>;
     return hd == 128 ? tree_attention_kernel<__half, 128> : tree_attention_kernel<__half, 64>;
@@ -134,10 +134,10 @@ bool make_page_map(CUtensorMap* m, const void* base, const sdv_pages* p, int box
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 int tree_blocks(int dev) { return min(kTreeBlocksPerSm * sm_count(dev), kTreeMaxBlocks); }
-// Workspace: tiles before every sequence | maxima and sums | outputs.
-size_t tree_bytes(int n_seqs, int head_dim, int blocks, int rows) {
+// Workspace: maxima and sums | outputs, of up to two partial items a block.
+size_t tree_bytes(int head_dim, int blocks, int rows) {
     const size_t parts = (size_t)blocks * 2 * rows;
-    return align256(((size_t)n_seqs + 1) * sizeof(long long)) + align256(parts * sizeof(float2)) + parts * head_dim * sizeof(float);
+    return align256(parts * sizeof(float2)) + parts * head_dim * sizeof(float);
 }
 
 }  // namespace
@@ -199,7 +199,7 @@ int sdv_rope_append(const sdv_rope_args* a, const sdv_pages* pages, void* cuda_s
 size_t sdv_tree_attention_workspace_bytes(int n_seqs, int head_dim) {
     int dev = 0;
     if (n_seqs < 0 || n_seqs > SDV_MAX_SEQUENCES || (head_dim != 64 && head_dim != 128) || cudaGetDevice(&dev) != cudaSuccess) return 0;
-    return tree_bytes(n_seqs, head_dim, tree_blocks(dev), kTreeTileRows);
+    return tree_bytes(head_dim, tree_blocks(dev), kTreeTileRows);
 }
 
 int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void* cuda_stream) {
@@ -224,12 +224,10 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     const long long keys = min((long long)a->table_width * pages->page_size, (long long)INT_MAX);
     const long long most = ((keys + kTreeKeys - 1) / kTreeKeys) * chunks * pages->n_kv_heads * min(a->n_seqs, a->n_rows);   // no more tiles than this
     P.blocks = (int)min((long long)tree_blocks(dev), most);
-    P.part_rows = (int)min(rows, (long long)kTreeTileRows);
-    if (a->workspace_bytes < tree_bytes(a->n_seqs, hd, P.blocks, P.part_rows)) return SDV_ENOMEM;
+    P.part_rows = (int)min((rows + 3) / 4 * 4, (long long)kTreeTileRows);   // in fours
+    if (a->workspace_bytes < tree_bytes(hd, P.blocks, P.part_rows)) return SDV_ENOMEM;
     const size_t parts = (size_t)P.blocks * 2 * P.part_rows;
     uint8_t* ws = (uint8_t*)a->workspace;
-    P.tiles_before = (long long*)ws;
-    ws += align256(((size_t)a->n_seqs + 1) * sizeof(long long));
     P.part_ml = (float2*)ws;
     P.part_o = (float*)(ws + align256(parts * sizeof(float2)));
     P.q = a->q;
@@ -263,10 +261,12 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     if (!make_page_map(&map_k, pages->k, pages, box_keys) || !make_page_map(&map_v, pages->v, pages, box_keys)) return SDV_EINVAL;
     const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, false, map_k, map_v, P);
     if (first != SDV_OK || P.blocks == 1) return first;   // one block does everything alone
-    // pairs of row and head that a merging block takes at a time: one while there are blocks to spare
-    const long long pairs = (long long)a->n_rows * a->n_q_heads, room = (long long)sm_count(dev) * 8;
-    const int group = (int)min((long long)kMergeWarps, (pairs + room - 1) / room);
-    return launch(merge_kernel(pages->dtype, hd), (int)min((pairs + group - 1) / group, room), kMergeThreads, 0, cuda_stream, 1, true, P, group);
+    // Merge: units of four (row, head) pairs (see tree_merge_kernel), of 32 columns each while that leaves no more than two blocks an SM; as many at a time for a block as
+    // that needs.
+    const long long units = (((long long)a->n_rows * g + 3) / 4 + a->n_seqs) * pages->n_kv_heads, room = (long long)sm_count(dev) * 2;
+    const int split = units * (hd / 32) <= room ? hd / 32 : 1;
+    const int group = (int)min((long long)kMergeWarps, (units * split + room - 1) / room);
+    return launch(merge_kernel(pages->dtype, hd), (int)min((units * split + group - 1) / group, room), kMergeThreads, 0, cuda_stream, 1, true, P, group, split);
 }
 
 int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {

@@ -28,14 +28,61 @@ struct TreeParams : TreeLists {
     void* out;
     const void* v;                     // pool, for values that are not finite
     const int *block_table, *parent;
-    long long* tiles_before;           // [n_seqs + 1] tiles of the sequences before, for the merge
-    float* part_o;                     // [block][2][part_rows][HD]
+    float* part_o;                     // [block][2][part_rows / 4][HD / 8][4][8]: four rows' 32 bytes make a line, for the storing warp and for the merge
     float2* part_ml;                   // [block][2][part_rows] maximum (log2 units), sum
     int* status;
     long long q_row_stride, q_head_stride, out_row_stride, out_head_stride, table_stride, page_stride, head_stride, token_stride;
     int page_shift, n_pages, part_rows, blocks;
     float scale_log2e;
     unsigned long long wait_limit_ns;
+};
+
+// Tiles of all sequences, summed up by a block: thread t has the sequences [t * per, (t + 1) * per).
+template <int WARPS>
+struct TreeScan {
+    long long warp_sum[WARPS], before[WARPS * 32];   // within its warp
+    __device__ __forceinline__ static int per(const TreeLists& P) { return (P.n_seqs + WARPS * 32 - 1) / (WARPS * 32); }
+    __device__ __forceinline__ void fill(const TreeLists& P) {   // all threads; a barrier follows
+        const int tid = threadIdx.x, lane = tid & 31, n = per(P), b0 = min(tid * n, P.n_seqs), b1 = min(b0 + n, P.n_seqs);
+        long long sum = 0;
+        for (int b = b0; b < b1; ++b) sum += tree_tiles(P, tree_seq(P, b));
+        long long incl = sum;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += v;
+        }
+        before[tid] = incl - sum;
+        if (lane == 31) warp_sum[tid >> 5] = incl;
+    }
+    __device__ __forceinline__ long long total() const {
+        long long t = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) t += warp_sum[w];
+        return t;
+    }
+    // Tiles of the sequences before sequence b.
+    __device__ __forceinline__ long long tiles_before(const TreeLists& P, int b) const {
+        const int n = per(P), t = b / n;
+        long long sum = before[t];
+        for (int w = 0; w < t >> 5; ++w) sum += warp_sum[w];
+        for (int k = t * n; k < b; ++k) sum += tree_tiles(P, tree_seq(P, k));
+        return sum;
+    }
+    // The sequence that has tile `tile` (below the total), and how far into it; whole warps.
+    __device__ __forceinline__ int find_tile(const TreeLists& P, long long& tile) const {
+        const int lane = threadIdx.x & 31;
+        int w = 0;
+        while (w < WARPS - 1 && tile >= warp_sum[w]) tile -= warp_sum[w++];
+        const int t = w * 32 + 31 - __clz(__ballot_sync(0xffffffffu, before[w * 32 + lane] <= tile));   // the last thread that begins at or before it
+        tile -= before[t];
+        int b = t * per(P);
+        for (;; ++b) {
+            const long long n = tree_tiles(P, tree_seq(P, b));
+            if (tile < n || b + 1 >= P.n_seqs) return b;
+            tile -= n;
+        }
+    }
 };
 
 __device__ __forceinline__ void tma_load_4d(void* smem_dst, const void* map, int x, int y, int z, int w, uint64_t* bar) {
@@ -123,10 +170,12 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     struct Ctl {
         uint64_t full[S::kSlots], empty[S::kSlots], s_full[2], p_ready[2], pv_done[2], q_ready, drained;
         unsigned long long bad[4];     // rows of the tree with values that are not finite, by item (modulo 4)
-        long long warp_sum[kTreeThreads / 32], total, offset;
         uint32_t tmem_base;
-        int abort_flag, b0;
+        int abort_flag;
     };
+    typedef TreeScan<kTreeThreads / 32> Scan;
+    Scan& scan = *reinterpret_cast<Scan*>(Qs);   // before there are queries
+    static_assert(sizeof(Scan) <= S::kQBytes, "sums over the sequences");
     Ctl* ctl = reinterpret_cast<Ctl*>(ring + S::kSlots * S::kSlotBytes);
     static_assert(sizeof(Ctl) <= S::kCtlBytes, "control block");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
@@ -147,45 +196,23 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         mbar_fence_init();
     }
     if (warp == 5) tmem_alloc(&ctl->tmem_base, 256);   // S0 | S1, 64 columns each | O, HD columns
-    // tiles of every sequence, summed up: each thread takes a run of sequences
-    const int B = P.n_seqs, per = (B + kTreeThreads - 1) / kTreeThreads, sb0 = min(tid * per, B), sb1 = min(sb0 + per, B);
-    long long sum = 0;
-    for (int b = sb0; b < sb1; ++b) sum += tree_tiles(P, tree_seq(P, b));
-    long long incl = sum;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, incl, off);
-        if (lane >= off) incl += v;
-    }
-    if (lane == 31) ctl->warp_sum[warp] = incl;
+    if (warp == 4 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &map_v : &map_k) : "memory");
+    scan.fill(P);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctl->tmem_base;
     grid_dep_launch();
-    long long before = incl - sum, total = 0;
-    for (int w = 0; w < kTreeThreads / 32; ++w) {
-        if (w < warp) before += ctl->warp_sum[w];
-        total += ctl->warp_sum[w];
-    }
+    const long long total = scan.total();
     const int sharers = tree_sharers(total, P.blocks);
     const long long my0 = tree_share(total, (int)blockIdx.x, sharers), my1 = tree_share(total, (int)blockIdx.x + 1, sharers);
-    if (blockIdx.x == 0 || (my0 < my1 && my0 >= before && my0 < before + sum)) {
-        long long at = before;
-        for (int b = sb0; b < sb1; ++b) {
-            const long long n = tree_tiles(P, tree_seq(P, b));
-            if (blockIdx.x == 0) P.tiles_before[b] = at;
-            if (my0 >= at && my0 < at + n) {
-                ctl->b0 = b;
-                ctl->offset = my0 - at;
-            }
-            at += n;
-        }
-        if (blockIdx.x == 0 && tid == kTreeThreads - 1) P.tiles_before[B] = total;
-    }
-    __syncthreads();
     TreeCursor cur;
-    cur.start(P, my0 < my1 ? ctl->b0 : 0, my0 < my1 ? ctl->offset : 0, my1 - my0);
+    {
+        long long offset = my0;
+        const int b0 = my0 < my1 ? scan.find_tile(P, offset) : 0;
+        cur.start(P, b0, offset, my1 - my0);
+    }
+    __syncthreads();   // the queries take the sums' place
 
     if (warp == 4) {
         // ---- copies: K0 V0 K1 V1 ... through the ring
@@ -308,21 +335,26 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         int mask_b = -1;
         unsigned long long anc0 = 0, anc1 = 0;
         uint32_t v_slot = 1, v_par = 0;
-        const auto load_q = [&](const TreeCursor& c) {   // the item's query rows; tile rows without one keep what they hold
+        // An item's query rows are copied asynchronously; tile rows without one keep what they hold.
+        const auto request_q = [&](const TreeCursor& c) {
             const int r = c.c * kTreeTileRows + t, j = r / P.g, hh = r - j * P.g;
             if (j < c.s.rows) {
-                const uint4* src = reinterpret_cast<const uint4*>((const T*)P.q + (c.s.first + j) * P.q_row_stride + (c.h * P.g + hh) * P.q_head_stride);
-                uint4 v[UNITS];
+                const T* src = (const T*)P.q + (c.s.first + j) * P.q_row_stride + (c.h * P.g + hh) * P.q_head_stride;
 #pragma unroll
-                for (int i = 0; i < UNITS; ++i) v[i] = __ldg(src + i);
-#pragma unroll
-                for (int i = 0; i < UNITS; ++i) *reinterpret_cast<uint4*>(Qs + (i >> 3) * (kTreeTileRows * 128) + swz_unit(t, i & 7)) = v[i];
+                for (int i = 0; i < UNITS; ++i) cp_async_16_zfill(Qs + (i >> 3) * (kTreeTileRows * 128) + swz_unit(t, i & 7), src + i * 8, true);
             }
+            cp_async_commit();
+        };
+        const auto announce_q = [&]() {
+            cp_async_wait<0>();
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl->q_ready);
         };
-        if (cur.left > 0) load_q(cur);
+        if (cur.left > 0) {
+            request_q(cur);
+            announce_q();
+        }
         while (cur.left > 0) {
             const int n = cur.run();
             const TreeSeq& sq = cur.s;
@@ -338,6 +370,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 see = j < 32 ? a0 : a1;
             }
             float m = -CUDART_INF_F, l = 0.f;
+            TreeCursor nxt = cur;
+            nxt.skip(P, n);
             for (int k = 0; k < n; ++k, ++n_t) {
                 const int key0 = (cur.tile + k) * kTreeKeys, new0 = sq.length - key0, left = sq.keys - key0;   // first new key, keys left, within the tile
                 const uint32_t ts = tmem + lanes + (n_t & 1u) * kTreeKeys;
@@ -371,6 +405,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
+                if (k == n - 1 && nxt.left > 0) request_q(nxt);   // the item's last scores are there: its queries are not needed any more
                 if (some) {
                     tc_fence_after();
                     uint32_t v[2][32];
@@ -438,11 +473,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 v_slot += 2;
                 if (v_slot >= S::kSlots) { v_slot -= S::kSlots; v_par ^= 1u; }
             }
-            // The scores of the item's last tile were read by every warp before it announced its probabilities, but a slower warp's queries may still be
-            // in use: they are not, once the scores are there (s_full of the last tile).  The next item's queries go in while P V finishes.
-            TreeCursor nxt = cur;
-            nxt.skip(P, n);
-            if (nxt.left > 0 && ok) load_q(nxt);
+            if (nxt.left > 0 && ok) announce_q();
             if (ok) ok = mbar_wait_bounded(&ctl->pv_done[(n_t - 1u) & 1u], ((n_t - 1u) >> 1) & 1u, &ctl->abort_flag, P.wait_limit_ns);
             ok = __all_sync(0xffffffffu, ok);
             const bool whole = n == sq.tiles;
@@ -450,7 +481,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 tc_fence_after();
                 const unsigned long long bad = *(volatile unsigned long long*)&ctl->bad[item & 3u] & see;
                 const int slot = (int)blockIdx.x * 2 + (item ? 1 : 0);   // an item that is not the block's first is its last, or whole
-                float* po = P.part_o + ((long long)slot * P.part_rows + t) * HD;
+                float* po = P.part_o + (long long)slot * P.part_rows * HD + (t >> 2) * (4 * HD) + (t & 3) * 8;
                 T* dst = (T*)P.out + (sq.first + j) * P.out_row_stride + (cur.h * P.g + hh) * P.out_head_stride;
                 const float sc = whole ? 1.f / l : 1.f;
                 if (!whole && real) P.part_ml[(long long)slot * P.part_rows + t] = ok ? make_float2(m, l) : make_float2(0.f, CUDART_NAN_F);
@@ -474,7 +505,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                                            Half16<T>::pack(__uint_as_float(o[i + 4]) * sc, __uint_as_float(o[i + 5]) * sc), Half16<T>::pack(__uint_as_float(o[i + 6]) * sc, __uint_as_float(o[i + 7]) * sc));
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) st_global_v8(po + c + i, o + i);
+                        for (int i = 0; i < 32; i += 8) st_global_v8(po + (c + i) * 4, o + i);
                     }
                 }
                 tc_fence_before();
@@ -491,128 +522,169 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     if (tid == 0 && ctl->abort_flag && P.status) atomicExch(P.status, 1);
 }
 
-// Output rows whose keys several blocks went through: un-normalised partial outputs weighted by 2^(maximum - largest maximum).  A block takes `group` pairs of row and
-// query head at a time; a pair with up to eight parts is one warp's, one with more the whole block's (a long cache of few sequences is cut into up to 150
-// parts: read by one warp, they would take longer than the attention).
-constexpr int kMergeThreads = 256, kMergeWarps = kMergeThreads / 32;
-struct TreePart {   // where the parts of an output row are
-    int block0, n, row;   // first block, blocks, tile row
+// Output rows whose keys several blocks went through: un-normalised partial outputs weighted by 2^(maximum - largest maximum).  The work is in units of four tile rows of an
+// item (of 32 columns each when `split`: where there are few units), a lane has four columns of one row.  A block takes `group` units at a time; one with up to four parts is one
+// warp's, one with more the whole block's (a long cache of few sequences is cut into up to 150 parts).  Where the parts are follows from the lengths alone
+// and is worked out before the attention is waited for.
+constexpr int kMergeWarps = 16, kMergeThreads = kMergeWarps * 32, kMergeFew = 4, kMergeDeep = 5;   // parts a warp has in flight
+struct TreeUnit {
+    int block0, n;        // first block with a part, parts
+    int row, rows;        // first tile row, rows
+    int b, h, j0;         // sequence, KV head, first (row, head of the group) of the unit within the sequence
+    int col0, cols;       // columns
     bool late;            // of block0 it is the second partial item
-    __device__ __forceinline__ long long at(const TreeParams& P, int i) const { return ((long long)(block0 + i) * 2 + (i == 0 && late ? 1 : 0)) * P.part_rows + row; }
+    __device__ __forceinline__ int slot(int i) const { return (block0 + i) * 2 + (i == 0 && late ? 1 : 0); }
 };
 
 template <typename T, int HD>
-__global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_constant__ TreeParams P, int group) {
-    constexpr int VEC = HD / 32;   // columns of a lane
-    __shared__ TreePart shared_part[kMergeWarps];
-    __shared__ float weight[kTreeMaxBlocks], red[kMergeWarps], sums[kMergeWarps][HD];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_q = P.n_kv * P.g, B = P.n_seqs;
-    const long long pairs = (long long)P.n_rows * n_q;
-    grid_dep_wait();
-    const long long total = P.tiles_before[B];
-    const auto store = [&](long long pair, const float (&o)[VEC], float sum) {
-        const int r = (int)(pair / n_q), hq = (int)(pair - (long long)r * n_q);
-        T* dst = (T*)P.out + r * P.out_row_stride + hq * P.out_head_stride + lane * VEC;
+__global__ void __launch_bounds__(kMergeThreads, 2) tree_merge_kernel(const __grid_constant__ TreeParams P, int group, int split) {
+    __shared__ TreeScan<kMergeWarps> scan;
+    __shared__ TreeUnit shared_unit[kMergeWarps];
+    __shared__ float4 shared_o[kMergeWarps][32];
+    __shared__ float2 shared_ml[kMergeWarps][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, my_row = (lane >> 1) & 3, my_col = (lane >> 3) * 8 + (lane & 1) * 4;
+    scan.fill(P);
+    __syncthreads();
+    const long long total = scan.total();
+    const int sharers = tree_sharers(total, P.blocks);
+    // units are numbered by the rows of the whole call: (row, query head) pairs of a KV head in fours, those of a sequence beginning a new one; sequence b's begin at
+    // ceil(first row * g / 4) + b
+    const long long units = ((long long)P.n_rows * P.g + 3) / 4 + P.n_seqs, tasks = units * P.n_kv * split;
+    bool waited = false;
+    // (at most 1024 blocks of two parts of 128 rows of 128 columns: offsets within 32 bits)
+    const int o_lane = (lane >> 3) * 32 + my_row * 8 + (lane & 1) * 4;
+    const auto ml_of = [&](const TreeUnit& q, int i) { return __ldcg(P.part_ml + q.slot(i) * P.part_rows + q.row + my_row); };
+    const auto o_of = [&](const TreeUnit& q, int i, int c) {
+        return __ldcg(reinterpret_cast<const float4*>(P.part_o + (q.slot(i) * P.part_rows + q.row) * HD + c * 4 + o_lane));
+    };
+    const auto store = [&](const TreeUnit& q, int c, const float4& o, float sum) {
+        const int r = q.j0 + my_row, j = r / P.g, hh = r - j * P.g;
+        if (my_row >= q.rows) return;
+        T* dst = (T*)P.out + (rows_begin(P.cu_rows, q.b, P.n_rows) + j) * P.out_row_stride + (q.h * P.g + hh) * P.out_head_stride + c + my_col;
         const float sc = 1.f / sum;
-        if constexpr (VEC == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(Half16<T>::pack(o[0] * sc, o[1] * sc), Half16<T>::pack(o[2] * sc, o[3] * sc));
-        else *reinterpret_cast<uint32_t*>(dst) = Half16<T>::pack(o[0] * sc, o[1] * sc);
+        *reinterpret_cast<uint2*>(dst) = make_uint2(Half16<T>::pack(o.x * sc, o.y * sc), Half16<T>::pack(o.z * sc, o.w * sc));
     };
-    const auto add = [&](float (&o)[VEC], float w, long long at) {
-        const float* src = P.part_o + at * HD + lane * VEC;
-        if constexpr (VEC == 4) {
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
-            o[0] += w * x.x; o[1] += w * x.y; o[2] += w * x.z; o[3] += w * x.w;
-        } else {
-            const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
-            o[0] += w * x.x; o[1] += w * x.y;
-        }
-    };
-    for (long long p0 = (long long)blockIdx.x * group; p0 < pairs; p0 += (long long)gridDim.x * group) {
-        TreePart part;
-        part.n = 0;
-        const long long pair = p0 + warp;
-        if (warp < group && pair < pairs && total > 0) {
-            const int r = (int)(pair / n_q), hq = (int)(pair - (long long)r * n_q);
-            // the row's sequence: the last one that begins at or before it, by two (for over 1024 sequences more) ballots
-            int lo = 0, n = B;   // among lo .. lo + n - 1
+    const auto add = [](float4& o, float w, const float4& x) { o.x += w * x.x; o.y += w * x.y; o.z += w * x.z; o.w += w * x.w; };
+    for (long long p0 = (long long)blockIdx.x * group; p0 < tasks; p0 += (long long)gridDim.x * group) {
+        TreeUnit q;
+        q.n = 0;
+        const long long task = p0 + warp;
+        if (warp < group && task < tasks && total > 0) {
+            const int part = (int)(task % split);
+            const long long u = task / split;
+            q.h = (int)(u % P.n_kv);
+            const long long unit = u / P.n_kv;
+            // the last sequence that begins at or before the unit, by ballots
+            int lo = 0, n = P.n_seqs;
             while (n > 1) {
                 const int step = (n + 31) / 32, at = lo + lane * step;
-                const bool begins = lane * step < n && rows_begin(P.cu_rows, at, P.n_rows) <= r;
+                const bool begins = lane * step < n && ((long long)rows_begin(P.cu_rows, at, P.n_rows) * P.g + 3) / 4 + at <= unit;
                 const int k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, begins)));
                 n = min(step, n - k * step);
                 lo += k * step;
             }
             const TreeSeq s = tree_seq(P, lo);
-            const int j = r - s.first;
-            if (j >= 0 && j < s.rows && s.tiles > 0) {
-                const int h = hq / P.g, tr = j * P.g + hq - h * P.g, c = tr / kTreeTileRows;
-                const long long tile0 = P.tiles_before[lo] + ((long long)h * s.chunks + c) * s.tiles;
-                const int sharers = tree_sharers(total, P.blocks);
-                part.block0 = tree_owner(total, tile0, sharers);
-                part.n = tree_owner(total, tile0 + s.tiles - 1, sharers) - part.block0 + 1;
-                part.row = tr - c * kTreeTileRows;
-                part.late = tree_share(total, part.block0, sharers) < tile0;
+            q.b = lo;
+            const long long j0 = (unit - (((long long)s.first * P.g + 3) / 4 + lo)) * 4;
+            if (j0 >= 0 && j0 < (long long)s.rows * P.g && s.tiles > 0) {
+                q.j0 = (int)j0;
+                q.rows = min(4, s.rows * P.g - q.j0);
+                const int c = q.j0 / kTreeTileRows;
+                const long long tile0 = scan.tiles_before(P, lo) + ((long long)q.h * s.chunks + c) * s.tiles;
+                q.block0 = tree_owner(total, tile0, sharers);
+                q.n = tree_owner(total, tile0 + s.tiles - 1, sharers) - q.block0 + 1;
+                q.row = q.j0 - c * kTreeTileRows;
+                q.late = tree_share(total, q.block0, sharers) < tile0;
+                q.cols = HD / split;
+                q.col0 = part * q.cols;
             }
         }
-        if (part.n > 1 && part.n <= 8) {
-            const float2 ml = lane < part.n ? __ldcg(P.part_ml + part.at(P, lane)) : make_float2(-CUDART_INF_F, 0.f);
-            float mx = ml.x;
+        if (lane == 0) shared_unit[warp] = q;
+        __syncwarp();
+        if (!waited) grid_dep_wait();   // the parts are there
+        waited = true;
+        const TreeUnit& mine = shared_unit[warp];
+        if (q.n > 1 && q.n <= kMergeFew) {
+            float2 ml[kMergeFew];
 #pragma unroll
-            for (int off = 4; off; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-            mx = __shfl_sync(0xffffffffu, mx, 0);
-            const float w = exp2f(ml.x - (mx == -CUDART_INF_F ? 0.f : mx));
-            float sum = w * ml.y;
+            for (int i = 0; i < kMergeFew; ++i) ml[i] = i < mine.n ? ml_of(mine, i) : make_float2(-CUDART_INF_F, 0.f);
+            const float mx = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), ref = mx == -CUDART_INF_F ? 0.f : mx;
+            float sum = 0.f;
 #pragma unroll
-            for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            float o[VEC] = {};
-            for (int i = 0; i < part.n; ++i) add(o, __shfl_sync(0xffffffffu, w, i), part.at(P, i));
-            store(pair, o, sum);
+            for (int i = 0; i < kMergeFew; ++i) {
+                ml[i].x = exp2f(ml[i].x - ref);
+                sum += ml[i].x * ml[i].y;
+            }
+#pragma unroll 2
+            for (int c = mine.col0; c < mine.col0 + mine.cols; c += 32) {
+                float4 x[kMergeFew], o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < kMergeFew; ++i)
+                    if (i < mine.n) x[i] = o_of(mine, i, c);
+#pragma unroll
+                for (int i = 0; i < kMergeFew; ++i)
+                    if (i < mine.n) add(o, ml[i].x, x[i]);
+                store(mine, c, o, sum);
+            }
         }
-        if (lane == 0) shared_part[warp] = part;
         __syncthreads();
         for (int k = 0; k < group; ++k) {
-            const TreePart q = shared_part[k];
-            if (q.n <= 8) continue;   // the same for the whole block
-            float mx = -CUDART_INF_F;
-            for (int i = threadIdx.x; i < q.n; i += kMergeThreads) mx = fmaxf(mx, __ldcg(P.part_ml + q.at(P, i)).x);
+            if (shared_unit[k].n <= kMergeFew) continue;   // the same for the whole block
+            const TreeUnit& w = shared_unit[k];
+            for (int c = w.col0; c < w.col0 + w.cols; c += 32) {
+                // a warp's parts: warp, warp + 16, ...
+                float m = -CUDART_INF_F, l = 0.f;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                constexpr int DEEP = kMergeDeep;
+#pragma unroll 1
+                for (int i0 = warp; i0 < w.n; i0 += DEEP * kMergeWarps) {
+                    float2 ml[DEEP];
+                    float4 x[DEEP];
 #pragma unroll
-            for (int off = 16; off; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-            if (lane == 0) red[warp] = mx;
-            __syncthreads();
+                    for (int t = 0; t < DEEP; ++t) {
+                        const int i = i0 + t * kMergeWarps;
+                        ml[t] = make_float2(-CUDART_INF_F, 0.f);
+                        if (i < w.n) {
+                            ml[t] = ml_of(w, i);
+                            x[t] = o_of(w, i, c);
+                        }
+                    }
+                    float mx = m;
 #pragma unroll
-            for (int w = 0; w < kMergeWarps; ++w) mx = fmaxf(mx, red[w]);
-            const float ref = mx == -CUDART_INF_F ? 0.f : mx;
-            float sum = 0.f;
-            for (int i = threadIdx.x; i < q.n; i += kMergeThreads) {
-                const float2 ml = __ldcg(P.part_ml + q.at(P, i));
-                weight[i] = exp2f(ml.x - ref);
-                sum += weight[i] * ml.y;
+                    for (int t = 0; t < DEEP; ++t) mx = fmaxf(mx, ml[t].x);
+                    const float ref = mx == -CUDART_INF_F ? 0.f : mx, keep = exp2f(m - ref);
+                    l *= keep;
+                    o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
+#pragma unroll
+                    for (int t = 0; t < DEEP; ++t)
+                        if (i0 + t * kMergeWarps < w.n) {
+                            const float f = exp2f(ml[t].x - ref);
+                            l += f * ml[t].y;
+                            add(o, f, x[t]);
+                        }
+                    m = mx;
+                }
+                shared_o[warp][lane] = o;
+                shared_ml[warp][lane] = make_float2(m, l);
+                __syncthreads();
+                if (warp == 0) {
+                    float mx = -CUDART_INF_F, sum = 0.f;
+#pragma unroll
+                    for (int t = 0; t < kMergeWarps; ++t) mx = fmaxf(mx, shared_ml[t][lane].x);
+                    const float ref = mx == -CUDART_INF_F ? 0.f : mx;
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int t = 0; t < kMergeWarps; ++t) {
+                        const float f = exp2f(shared_ml[t][lane].x - ref);
+                        sum += f * shared_ml[t][lane].y;
+                        add(v, f, shared_o[t][lane]);
+                    }
+                    store(w, c, v, sum);
+                }
+                __syncthreads();
             }
-#pragma unroll
-            for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            __syncthreads();   // the maxima have been read
-            if (lane == 0) red[warp] = sum;
-            __syncthreads();
-            sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < kMergeWarps; ++w) sum += red[w];
-            float o[VEC] = {};
-#pragma unroll 8
-            for (int i = warp; i < q.n; i += kMergeWarps) add(o, weight[i], q.at(P, i));
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) sums[warp][lane * VEC + v] = o[v];
-            __syncthreads();
-            if (warp == 0) {
-                float t[VEC] = {};
-#pragma unroll
-                for (int w = 0; w < kMergeWarps; ++w)
-#pragma unroll
-                    for (int v = 0; v < VEC; ++v) t[v] += sums[w][lane * VEC + v];
-                store(p0 + k, t, sum);
-            }
-            __syncthreads();
         }
-        __syncthreads();   // shared_part is read before the next pairs'
+        __syncthreads();   // shared_unit is read before the next units'
     }
 }
 

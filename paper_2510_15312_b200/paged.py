@@ -8,7 +8,10 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import math
-from typing import Optional, Tuple
+import struct
+from typing import Optional
+
+import torch
 
 from . import binding
 from .binding import EINVAL, OK, SdvError
@@ -45,46 +48,60 @@ class _VerifyArgs(C.Structure):
                                    "out_slots")] + [("target_stride", _ll), ("draft_stride", _ll)] + [(n, _i) for n in ("n_seqs", "n_rows", "vocab")]
 
 
-_types = None   # torch dtype -> SDV_BF16 / SDV_FP16
+def _packer(structure):
+    """Packs a structure's fields, in order, into bytes with the structure's layout (a fifth of the time that filling a ctypes structure takes)."""
+    code = {_vp: "P", _i: "i", _ll: "q", _f: "f", C.c_size_t: "N"}
+    s = struct.Struct("@" + "".join(code[t] for _, t in structure._fields_))
+    assert s.size <= C.sizeof(structure) <= s.size + 7   # the padding at the end is nobody's field
+    return struct.Struct(s.format + "0q").pack
+
+
+_pack_pages, _pack_slots, _pack_rope, _pack_attention, _pack_verify = (_packer(t) for t in (_Pages, _SlotsArgs, _RopeArgs, _AttentionArgs, _VerifyArgs))
+_i32 = torch.int32
+_types = {torch.bfloat16: 0, torch.float16: 1}   # SDV_BF16, SDV_FP16
+_no_context = contextlib.nullcontext()
+_present = False                                 # whether a CUDA device has been seen
 
 
 def _dtype(t, what: str) -> int:
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.bfloat16: 0, torch.float16: 1}
     d = _types.get(t.dtype)
     if d is None:
         raise ValueError(f"{what}: bfloat16 or float16 expected, got {t.dtype}")
     return d
 
 
-def _index(t, shape: Tuple[int, ...], what: str, device: int) -> int:
+def _index(t, shape, device: int, what: str) -> int:
     """Address of a contiguous int32 tensor of this shape on the device."""
-    import torch
-    if t.dtype is not torch.int32 or t.get_device() != device or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not _i32 or t.get_device() != device or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous int32 tensor of shape {tuple(shape)} on the current device expected")
     return t.data_ptr()
 
 
-def _on(t, device: int, what: str):
-    if t.get_device() != device:
-        raise ValueError(f"{what}: not on the current CUDA device")
+def _table(t, n: int, device: int):
+    """(address, width, distance of rows) of the block tables of n sequences."""
+    if t.dtype is not _i32 or t.get_device() != device or t.dim() != 2:
+        raise ValueError("block_table: int32 [sequences][width] on the current device expected")
+    rows, width = t.shape
+    row, column = t.stride()
+    if rows != n or (column != 1 and width > 1):
+        raise ValueError("block_table: a contiguous row for every sequence expected")
+    return t.data_ptr(), width, row if n > 1 else width
 
 
 def _enter(stream):
-    """(torch, current device, handle of the stream, context in which outputs are allocated)."""
-    import torch
-    if not torch.cuda.is_available():
-        raise SdvError(binding.ECUDA, "no CUDA device (there is no CPU fallback)")
+    """(current device, handle of the stream, context in which outputs are allocated)."""
+    global _present
+    if not _present:
+        if not torch.cuda.is_available():
+            raise SdvError(binding.ECUDA, "no CUDA device (there is no CPU fallback)")
+        _present = True
     device = torch.cuda.current_device()
     if stream is not None:
-        return torch, device, stream.cuda_stream, torch.cuda.stream(stream)
-    try:
-        s = torch._C._cuda_getCurrentRawStream(device)
+        return device, stream.cuda_stream, torch.cuda.stream(stream)
+    try:   # the current stream's handle without a Stream object around it, where torch has the function for it
+        return device, torch._C._cuda_getCurrentRawStream(device), _no_context
     except AttributeError:
-        s = torch.cuda.current_stream().cuda_stream
-    return torch, device, s, contextlib.nullcontext()
+        return device, torch.cuda.current_stream().cuda_stream, _no_context
 
 
 def _check(rc: int, where: str):
@@ -92,58 +109,55 @@ def _check(rc: int, where: str):
         raise SdvError(rc, where)
 
 
-def _pool(k_pages, v_pages, device: int) -> _Pages:
-    """[pages][KV heads][tokens of a page][head dim], any strides with contiguous head elements (a pool that keeps the
-    tokens outside the heads is passed as .transpose(1, 2))."""
-    if k_pages.ndim != 4 or v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype or v_pages.stride() != k_pages.stride():
+def _pool(k_pages, v_pages, device: int):
+    """(address of k, of v, type, pages, page size, KV heads, head dim, strides) of [pages][KV heads][tokens of a page][head dim], any strides with contiguous
+    head elements (a pool that keeps the tokens outside the heads is passed as .transpose(1, 2))."""
+    shape, strides, dtype = k_pages.shape, k_pages.stride(), k_pages.dtype
+    if len(shape) != 4 or v_pages.shape != shape or v_pages.dtype is not dtype or v_pages.stride() != strides:
         raise ValueError("k_pages and v_pages: two tensors [pages][KV heads][page size][head dim] of the same shape, strides and type expected")
-    _on(k_pages, device, "k_pages")
-    _on(v_pages, device, "v_pages")
-    n, heads, page, dim = k_pages.shape
-    s0, s1, s2, s3 = k_pages.stride()
+    if k_pages.get_device() != device or v_pages.get_device() != device:
+        raise ValueError("k_pages, v_pages: not on the current CUDA device")
+    n, heads, page, dim = shape
+    s0, s1, s2, s3 = strides
     if s3 != 1 and dim > 1:
         raise ValueError("k_pages: the elements of a head have to be contiguous")
     # the stride of a dimension of one says nothing
-    return _Pages(k_pages.data_ptr(), v_pages.data_ptr(), _dtype(k_pages, "k_pages"), n, page, heads, dim, s0 if n > 1 else 0, s1 if heads > 1 else 0, s2 if page > 1 else 0)
+    return (k_pages.data_ptr(), v_pages.data_ptr(), _dtype(k_pages, "k_pages"), n, page, heads, dim, s0 if n > 1 else 0, s1 if heads > 1 else 0, s2 if page > 1 else 0)
 
 
-def _rows(t, heads_dim, what: str, device: int):
-    """Row and head stride of a tensor [rows][heads][head dim]."""
-    if t.ndim != 3:
-        raise ValueError(f"{what}: [rows][heads][head dim] expected")
-    _on(t, device, what)
-    if t.shape[2] > 1 and t.stride(2) != 1:
+def _rows(t, device: int, what: str):
+    """(shape, row stride, head stride) of a tensor [rows][heads][head dim]."""
+    shape = t.shape
+    if len(shape) != 3 or t.get_device() != device:
+        raise ValueError(f"{what}: [rows][heads][head dim] on the current CUDA device expected")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and shape[2] > 1:
         raise ValueError(f"{what}: the elements of a head have to be contiguous")
-    if heads_dim is not None and (t.shape != heads_dim[0] or t.dtype != heads_dim[1]):
-        raise ValueError(f"{what}: shape {tuple(heads_dim[0])} of {heads_dim[1]} expected")
-    return (t.stride(0) if t.shape[0] > 1 else 0), (t.stride(1) if t.shape[1] > 1 else 0)
+    return shape, (s0 if shape[0] > 1 else 0), (s1 if shape[1] > 1 else 0)
 
 
 def paged_slots(kv_len, cu_rows, block_table, n_held, free_pages, free_state, page_size: int, n_rows: int, parent=None, out=None, stream=None):
     """Hands pages to the sequences that need more and gives every row its slot and position: (slots, positions, n_held, free_state) after the call;
     block_table [sequences][width] is updated in place.  free_state[0] is the first unused entry of free_pages; of the returned one, the second entry is the number of
     sequences that were refused for want of pages (their slots are -1).  out: the four tensors to write to."""
-    torch, dev, s, alloc = _enter(stream)
+    dev, s, alloc = _enter(stream)
     n = kv_len.shape[0]
-    if block_table.ndim != 2 or block_table.shape[0] != n or block_table.dtype is not torch.int32 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
-        raise ValueError("block_table: int32 [sequences][width] with contiguous rows expected")
-    _on(block_table, dev, "block_table")
-    n_rows = int(n_rows)
-    if n_rows < 0 or free_state.ndim != 1 or free_state.shape[0] < 1:
-        raise ValueError("paged_slots: n_rows >= 0 and a free_state of at least one entry expected")
+    table, width, table_stride = _table(block_table, n, dev)
+    if n_rows < 0 or free_state.dim() != 1 or free_state.shape[0] < 1 or free_pages.dim() != 1:
+        raise ValueError("paged_slots: n_rows >= 0, a list of free pages and a free_state of at least one entry expected")
+    per_row, per_seq = (n_rows,), (n,)
     if out is None:
+        device = kv_len.device
         with alloc:
-            both = torch.empty((2, n_rows), dtype=torch.int32, device=kv_len.device)
-            held = torch.empty(n + 2, dtype=torch.int32, device=kv_len.device)
-        out = (both[0], both[1], held[:n], held[n:])
+            out = (torch.empty(n_rows, dtype=_i32, device=device), torch.empty(n_rows, dtype=_i32, device=device), torch.empty(n, dtype=_i32, device=device),
+                   torch.empty(2, dtype=_i32, device=device))
     slots, positions, held, free = out
-    a = _SlotsArgs(_index(kv_len, (n,), "kv_len", dev), _index(cu_rows, (n + 1,), "cu_rows", dev), None if parent is None else _index(parent, (n_rows,), "parent", dev),
-                   _index(n_held, (n,), "n_held", dev), _index(free_pages, (free_pages.numel(),), "free_pages", dev), _index(free_state, free_state.shape, "free_state", dev),
-                   block_table.data_ptr(), _index(slots, (n_rows,), "slots", dev), _index(positions, (n_rows,), "positions", dev), _index(held, (n,), "n_held (out)", dev),
-                   _index(free, (2,), "free_state (out)", dev), block_table.stride(0) if n > 1 else block_table.shape[1], n, n_rows, page_size, block_table.shape[1],
-                   free_pages.numel())
-    _check(binding.lib().sdv_paged_slots(C.byref(a), s), "sdv_paged_slots")
-    return slots, positions, held, free
+    a = _pack_slots(_index(kv_len, per_seq, dev, "kv_len"), _index(cu_rows, (n + 1,), dev, "cu_rows"), 0 if parent is None else _index(parent, per_row, dev, "parent"),
+                    _index(n_held, per_seq, dev, "n_held"), _index(free_pages, free_pages.shape, dev, "free_pages"), _index(free_state, free_state.shape, dev, "free_state"), table,
+                    _index(slots, per_row, dev, "slots"), _index(positions, per_row, dev, "positions"), _index(held, per_seq, dev, "n_held (out)"),
+                    _index(free, (2,), dev, "free_state (out)"), table_stride, n, n_rows, page_size, width, free_pages.shape[0])
+    _check(binding.lib().sdv_paged_slots(a, s), "sdv_paged_slots")
+    return out
 
 
 def rope_frequencies(rot_dim: int, theta: float = 1.0e4, scaling: Optional[str] = None, factor: float = 1.0, original_positions: int = 8192, low: float = 1.0, high: float = 4.0,
@@ -181,44 +195,47 @@ def rope_append(positions, frequencies, q=None, k=None, v=None, k_pages=None, v_
     """Rotates q [rows][query heads][head dim] and k [rows][KV heads][head dim] by positions [rows] (int32) times frequencies [rot_dim / 2] (float64); k and v go to their
     slots of the pages, a row whose slot is outside the pool is not written.  q, or k, v, the pages and slots, may be left out.  Returns the rotated q (q_out; may be q
     itself), None without q."""
-    torch, dev, s, alloc = _enter(stream)
+    dev, s, alloc = _enter(stream)
     n = positions.shape[0]
-    if frequencies.dtype is not torch.float64 or frequencies.ndim != 1 or not frequencies.is_contiguous():
-        raise ValueError("frequencies: contiguous float64 [rot_dim / 2] expected")
-    _on(frequencies, dev, "frequencies")
-    first = q if q is not None else k
-    if first is None or (k is None) != (v is None):
+    per_row = (n,)
+    if frequencies.dtype is not torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous() or frequencies.get_device() != dev:
+        raise ValueError("frequencies: contiguous float64 [rot_dim / 2] on the current device expected")
+    if (q is None and k is None) or (k is None) != (v is None):
         raise ValueError("rope_append: q, or k and v, expected")
-    a = _RopeArgs(positions=_index(positions, (n,), "positions", dev), frequencies=frequencies.data_ptr(), n_rows=n, head_dim=first.shape[-1], rot_dim=2 * frequencies.shape[0],
-                  interleaved=bool(interleaved), dtype=_dtype(first, "q" if q is not None else "k"), factor=factor)
-    pages = None
-    if q is not None:
-        a.q_row_stride, a.q_head_stride = _rows(q, None, "q", dev)
-        if q.shape[0] != n:
-            raise ValueError("q: as many rows as positions expected")
-        if q_out is None:
-            with alloc:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        a.out_row_stride, a.out_head_stride = _rows(q_out, (q.shape, q.dtype), "q_out", dev)
-        a.q, a.q_out, a.n_q_heads = q.data_ptr(), q_out.data_ptr(), q.shape[1]
+    pages, q_ptr, out_ptr, k_ptr, v_ptr, slot_ptr = None, 0, 0, 0, 0, 0
+    q_row = q_head = out_row = out_head = k_row = k_head = v_row = v_head = heads = kv_heads = 0
     if k is not None:
         if k_pages is None or v_pages is None or slots is None:
             raise ValueError("rope_append: k and v need k_pages, v_pages and slots")
         pages = _pool(k_pages, v_pages, dev)
-        shape = torch.Size((n, pages.n_kv_heads, pages.head_dim))
-        a.k_row_stride, a.k_head_stride = _rows(k, (shape, k_pages.dtype), "k", dev)
-        a.v_row_stride, a.v_head_stride = _rows(v, (shape, k_pages.dtype), "v", dev)
-        a.k, a.v, a.slots, a.n_kv_heads = k.data_ptr(), v.data_ptr(), _index(slots, (n,), "slots", dev), pages.n_kv_heads
-        if q is not None and (q.dtype != k.dtype or q.shape[2] != k.shape[2]):
-            raise ValueError("rope_append: q and k of one type and head dim expected")
+        dtype, kv_heads, dim = pages[2], pages[5], pages[6]
+        shape, k_row, k_head = _rows(k, dev, "k")
+        v_shape, v_row, v_head = _rows(v, dev, "v")
+        if shape != (n, kv_heads, dim) or v_shape != shape or k.dtype is not k_pages.dtype or v.dtype is not k_pages.dtype:
+            raise ValueError("k, v: [rows][KV heads][head dim] of the pages' type expected")
+        k_ptr, v_ptr, slot_ptr = k.data_ptr(), v.data_ptr(), _index(slots, per_row, dev, "slots")
+    if q is not None:
+        shape, q_row, q_head = _rows(q, dev, "q")
+        if shape[0] != n or (k is not None and (shape[2] != dim or q.dtype is not k.dtype)):
+            raise ValueError("q: a row for every position, with the head dim and type of k, expected")
+        dtype, heads, dim = _dtype(q, "q"), shape[1], shape[2]
+        if q_out is None:
+            with alloc:
+                q_out = torch.empty_like(q)
+        out_shape, out_row, out_head = _rows(q_out, dev, "q_out")
+        if out_shape != shape or q_out.dtype is not q.dtype:
+            raise ValueError("q_out: shape and type of q expected")
+        q_ptr, out_ptr = q.data_ptr(), q_out.data_ptr()
+    half = frequencies.shape[0]
+    a = _pack_rope(q_ptr, k_ptr, v_ptr, out_ptr, _index(positions, per_row, dev, "positions"), slot_ptr, frequencies.data_ptr(), q_row, q_head, out_row, out_head, k_row, k_head,
+                   v_row, v_head, n, heads, kv_heads, dim, 2 * half, 1 if interleaved else 0, dtype, factor)
     if n:
-        _check(binding.lib().sdv_rope_append(C.byref(a), None if pages is None else C.byref(pages), s), "sdv_rope_append")
+        _check(binding.lib().sdv_rope_append(a, None if pages is None else _pack_pages(*pages), s), "sdv_rope_append")
     return q_out if q is not None else None
 
 
 def tree_attention_workspace(n_seqs: int, head_dim: int):
     """A workspace for tree_attention on the current device, for up to n_seqs sequences."""
-    import torch
     _enter(None)
     n = binding.lib().sdv_tree_attention_workspace_bytes(n_seqs, head_dim)
     if n == 0:
@@ -230,61 +247,67 @@ def tree_attention(q, k_pages, v_pages, block_table, kv_len, cu_rows, parent=Non
     """Every row of q [rows][query heads][head dim] attends to the kv_len[b] committed tokens of its sequence and to the rows on its own path through
     the draft tree, whose keys and values were appended before.  scale: 1 / sqrt(head dim) unless given.  out: like q; rows of no sequence are left as they were.  workspace: see
     tree_attention_workspace; without one torch allocates it for the call.  status: int32 [1], set to 1 when a wait inside the kernel ran out."""
-    torch, dev, s, alloc = _enter(stream)
+    dev, s, alloc = _enter(stream)
     pages = _pool(k_pages, v_pages, dev)
-    n, heads, dim = q.shape if q.ndim == 3 else (0, 0, 0)
-    q_row, q_head = _rows(q, None, "q", dev)
-    if q.dtype != k_pages.dtype or dim != pages.head_dim:
+    shape, q_row, q_head = _rows(q, dev, "q")
+    n, heads, dim = shape
+    if q.dtype is not k_pages.dtype or dim != pages[6]:
         raise ValueError("q: type and head dim of the pages expected")
     seqs = kv_len.shape[0]
-    if block_table.ndim != 2 or block_table.shape[0] != seqs or block_table.dtype is not torch.int32 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
-        raise ValueError("block_table: int32 [sequences][width] with contiguous rows expected")
-    _on(block_table, dev, "block_table")
+    table, width, table_stride = _table(block_table, seqs, dev)
     lib = binding.lib()
     with alloc:
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty_like(q)
         if workspace is None:
             workspace = torch.empty(lib.sdv_tree_attention_workspace_bytes(seqs, dim), dtype=torch.uint8, device=q.device)
-    out_row, out_head = _rows(out, (q.shape, q.dtype), "out", dev)
-    _on(workspace, dev, "workspace")
-    if n == 0 or seqs == 0:
-        return out
-    a = _AttentionArgs(q.data_ptr(), out.data_ptr(), block_table.data_ptr(), _index(kv_len, (seqs,), "kv_len", dev), _index(cu_rows, (seqs + 1,), "cu_rows", dev),
-                       None if parent is None else _index(parent, (n,), "parent", dev), workspace.data_ptr(),
-                       None if status is None else _index(status, (1,), "status", dev), workspace.numel() * workspace.element_size(), q_row, q_head, out_row, out_head,
-                       block_table.stride(0) if seqs > 1 else block_table.shape[1], seqs, n, heads, block_table.shape[1], dim ** -0.5 if scale is None else scale)
-    _check(lib.sdv_tree_attention(C.byref(a), C.byref(pages), s), "sdv_tree_attention")
+    out_shape, out_row, out_head = _rows(out, dev, "out")
+    if out_shape != shape or out.dtype is not q.dtype or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("out: shape and type of q, workspace: contiguous memory of the current device expected")
+    a = _pack_attention(q.data_ptr(), out.data_ptr(), table, _index(kv_len, (seqs,), dev, "kv_len"), _index(cu_rows, (seqs + 1,), dev, "cu_rows"),
+                        0 if parent is None else _index(parent, (n,), dev, "parent"), workspace.data_ptr(), 0 if status is None else _index(status, (1,), dev, "status"),
+                        workspace.numel() * workspace.element_size(), q_row, q_head, out_row, out_head, table_stride, seqs, n, heads, width, dim ** -0.5 if scale is None else scale)
+    if n and seqs:
+        _check(lib.sdv_tree_attention(a, _pack_pages(*pages), s), "sdv_tree_attention")
     return out
+
+
+def _probs(t, n: int, vocab: int, device: int, what: str):
+    """(address, distance of rows) of float32 [rows][vocab]."""
+    if t.dtype is not torch.float32 or t.get_device() != device or t.shape != (n, vocab):
+        raise ValueError(f"{what}: float32 [rows][vocab] on the current device expected")
+    row, column = t.stride()
+    if column != 1 and vocab > 1:
+        raise ValueError(f"{what}: contiguous rows expected")
+    return t.data_ptr(), row if n > 1 else vocab
 
 
 def verify_sampled(target_probs, tokens, cu_rows, uniforms, draft_probs=None, parent=None, slots=None, out=None, stream=None):
     """Accepts drafted tokens against the target's probabilities [rows][vocab] (float32) with the uniform random numbers uniforms [rows] and draws one
     token behind the accepted ones: (accept_len [sequences], tokens [rows], rows [rows], slots [rows] or None).  draft_probs [rows][vocab]: what each draft of a chain was sampled from; without, drafts
     count as certain (retrieved), and parent may make them trees.  slots: every row's slot, for the slots that accepted rows move to.  out: the tensors to write to."""
-    torch, dev, s, alloc = _enter(stream)
+    dev, s, alloc = _enter(stream)
     n, seqs = tokens.shape[0], cu_rows.shape[0] - 1
-    for t, what in ((target_probs, "target_probs"), (draft_probs, "draft_probs")):
-        if t is None:
-            continue
-        if t.ndim != 2 or t.dtype is not torch.float32 or t.shape != (n, target_probs.shape[1]) or (t.shape[1] > 1 and t.stride(1) != 1):
-            raise ValueError(f"{what}: float32 [rows][vocab] with contiguous rows expected")
-        _on(t, dev, what)
-    if uniforms.dtype is not torch.float32 or uniforms.shape != (n,) or not uniforms.is_contiguous() or uniforms.get_device() != dev:
-        raise ValueError("uniforms: contiguous float32 [rows] on the current device expected")
+    if target_probs.dim() != 2 or seqs < 0:
+        raise ValueError("verify_sampled: target_probs [rows][vocab] and cu_rows [sequences + 1] expected")
+    vocab = target_probs.shape[1]
+    target, target_stride = _probs(target_probs, n, vocab, dev, "target_probs")
+    draft, draft_stride = (0, 0) if draft_probs is None else _probs(draft_probs, n, vocab, dev, "draft_probs")
     if draft_probs is not None and parent is not None:
         raise ValueError("verify_sampled: drafts with probabilities are chains")
+    per_row = (n,)
+    if uniforms.dtype is not torch.float32 or uniforms.shape != per_row or not uniforms.is_contiguous() or uniforms.get_device() != dev:
+        raise ValueError("uniforms: contiguous float32 [rows] on the current device expected")
     if out is None:
+        device = tokens.device
         with alloc:
-            o = torch.empty(max(seqs, 0) + 3 * n, dtype=torch.int32, device=tokens.device)
-        out = (o[:seqs], o[seqs:seqs + n], o[seqs + n:seqs + 2 * n], None if slots is None else o[seqs + 2 * n:])
+            out = (torch.empty(seqs, dtype=_i32, device=device), torch.empty(n, dtype=_i32, device=device), torch.empty(n, dtype=_i32, device=device),
+                   None if slots is None else torch.empty(n, dtype=_i32, device=device))
     accept, out_tokens, out_rows, out_slots = out
-    vocab = target_probs.shape[1]
-    a = _VerifyArgs(target_probs.data_ptr(), None if draft_probs is None else draft_probs.data_ptr(), _index(tokens, (n,), "tokens", dev), _index(cu_rows, (seqs + 1,), "cu_rows", dev),
-                    None if parent is None else _index(parent, (n,), "parent", dev), None if slots is None else _index(slots, (n,), "slots", dev), uniforms.data_ptr(),
-                    _index(accept, (seqs,), "accept_len", dev), _index(out_tokens, (n,), "tokens (out)", dev), _index(out_rows, (n,), "rows (out)", dev),
-                    None if slots is None else _index(out_slots, (n,), "slots (out)", dev), target_probs.stride(0) if n > 1 else vocab,
-                    0 if draft_probs is None else draft_probs.stride(0) if n > 1 else vocab, seqs, n, vocab)
+    a = _pack_verify(target, draft, _index(tokens, per_row, dev, "tokens"), _index(cu_rows, (seqs + 1,), dev, "cu_rows"), 0 if parent is None else _index(parent, per_row, dev, "parent"),
+                     0 if slots is None else _index(slots, per_row, dev, "slots"), uniforms.data_ptr(), _index(accept, (seqs,), dev, "accept_len"),
+                     _index(out_tokens, per_row, dev, "tokens (out)"), _index(out_rows, per_row, dev, "rows (out)"), 0 if slots is None else _index(out_slots, per_row, dev, "slots (out)"),
+                     target_stride, draft_stride, seqs, n, vocab)
     if n and seqs:
-        _check(binding.lib().sdv_verify_sampled(C.byref(a), s), "sdv_verify_sampled")
-    return accept, out_tokens, out_rows, out_slots
+        _check(binding.lib().sdv_verify_sampled(a, s), "sdv_verify_sampled")
+    return out
