@@ -221,6 +221,8 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     memset(&P, 0, sizeof(P));
     const int hd = pages->head_dim, g = a->n_q_heads / pages->n_kv_heads;
     const long long rows = (long long)min(a->n_rows, SDV_TREE_ROWS) * g, chunks = (rows + kTreeTileRows - 1) / kTreeTileRows;
+    const long long units = (((long long)a->n_rows * g + 3) / 4 + a->n_seqs) * pages->n_kv_heads;   // of the merge
+    if ((long long)a->n_rows * a->n_q_heads > INT_MAX / 2 || units * (hd / 32) > INT_MAX) return SDV_EINVAL;
     const long long keys = min((long long)a->table_width * pages->page_size, (long long)INT_MAX);
     const long long most = ((keys + kTreeKeys - 1) / kTreeKeys) * chunks * pages->n_kv_heads * min(a->n_seqs, a->n_rows);   // no more tiles than this
     P.blocks = (int)min((long long)tree_blocks(dev), most);
@@ -261,9 +263,9 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     if (!make_page_map(&map_k, pages->k, pages, box_keys) || !make_page_map(&map_v, pages->v, pages, box_keys)) return SDV_EINVAL;
     const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, false, map_k, map_v, P);
     if (first != SDV_OK || P.blocks == 1) return first;   // one block does everything alone
-    // Merge: units of four (row, head) pairs (see tree_merge_kernel), of 32 columns each while that leaves no more than two blocks an SM; as many at a time for a block as
-    // that needs.
-    const long long units = (((long long)a->n_rows * g + 3) / 4 + a->n_seqs) * pages->n_kv_heads, room = (long long)sm_count(dev) * 2;
+    // Merge: units of four (row, head) pairs, of 32 columns where that leaves no more than two blocks an SM (see tree_merge_kernel); as many at a time for a block
+    // as two blocks an SM need.
+    const long long room = (long long)sm_count(dev) * 2;
     const int split = units * (hd / 32) <= room ? hd / 32 : 1;
     const int group = (int)min((long long)kMergeWarps, (units * split + room - 1) / room);
     return launch(merge_kernel(pages->dtype, hd), (int)min((units * split + group - 1) / group, room), kMergeThreads, 0, cuda_stream, 1, true, P, group, split);
@@ -280,10 +282,10 @@ int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {
     if ((a->draft && !on_device(a->draft, dev, 4)) || (a->parent && !on_device(a->parent, dev, 4)) || (a->slots && !on_device({a->slots, a->out_slots}, dev, 4))) return SDV_EINVAL;
     const int rc = prepare_device(dev);
     if (rc != SDV_OK) return rc;
-    // blocks that share a sequence's vocabulary: doubled while every warp keeps a tile and about four blocks an SM are not exceeded
+    // blocks that share a sequence's vocabulary: doubled while every warp keeps a tile and all blocks are resident at once (two an SM)
     const int tiles = (a->vocab + kVerifyTile - 1) / kVerifyTile;
     int cs = 1;
-    while (cs < kVerifyMaxCluster && tiles >= 2 * cs * kVerifyWarps && (long long)a->n_seqs * cs * 2 <= 4ll * sm_count(dev)) cs *= 2;
+    while (cs < kVerifyMaxCluster && tiles >= 2 * cs * kVerifyWarps && (long long)a->n_seqs * cs * 2 <= 2ll * sm_count(dev)) cs *= 2;
     const int per = (tiles + cs - 1) / cs;
     return launch(verify_sampled_kernel, a->n_seqs * cs, kVerifyThreads, (size_t)per * sizeof(double), cuda_stream, cs, false, *a, per);
 }

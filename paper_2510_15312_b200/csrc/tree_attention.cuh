@@ -28,8 +28,8 @@ struct TreeParams : TreeLists {
     void* out;
     const void* v;                     // pool, for values that are not finite
     const int *block_table, *parent;
-    float* part_o;                     // [block][2][part_rows / 4][HD / 8][4][8]: four rows' 32 bytes make a line, for the storing warp and for the merge
-    float2* part_ml;                   // [block][2][part_rows] maximum (log2 units), sum
+    float* part_o;                     // [2][block][part_rows / 4][HD / 8][4][8]: four rows' 32 bytes make a line, for the storing warp and for the merge
+    float2* part_ml;                   // [2][block][part_rows] maximum (log2 units), sum
     int* status;
     long long q_row_stride, q_head_stride, out_row_stride, out_head_stride, table_stride, page_stride, head_stride, token_stride;
     int page_shift, n_pages, part_rows, blocks;
@@ -40,7 +40,7 @@ struct TreeParams : TreeLists {
 // Tiles of all sequences, summed up by a block: thread t has the sequences [t * per, (t + 1) * per).
 template <int WARPS>
 struct TreeScan {
-    long long warp_sum[WARPS], before[WARPS * 32];   // within its warp
+    long long warp_sum[WARPS], before[WARPS * 32];   // before: within its warp
     __device__ __forceinline__ static int per(const TreeLists& P) { return (P.n_seqs + WARPS * 32 - 1) / (WARPS * 32); }
     __device__ __forceinline__ void fill(const TreeLists& P) {   // all threads; a barrier follows
         const int tid = threadIdx.x, lane = tid & 31, n = per(P), b0 = min(tid * n, P.n_seqs), b1 = min(b0 + n, P.n_seqs);
@@ -60,14 +60,6 @@ struct TreeScan {
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) t += warp_sum[w];
         return t;
-    }
-    // Tiles of the sequences before sequence b.
-    __device__ __forceinline__ long long tiles_before(const TreeLists& P, int b) const {
-        const int n = per(P), t = b / n;
-        long long sum = before[t];
-        for (int w = 0; w < t >> 5; ++w) sum += warp_sum[w];
-        for (int k = t * n; k < b; ++k) sum += tree_tiles(P, tree_seq(P, k));
-        return sum;
     }
     // The sequence that has tile `tile` (below the total), and how far into it; whole warps.
     __device__ __forceinline__ int find_tile(const TreeLists& P, long long& tile) const {
@@ -480,7 +472,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             if (some) {
                 tc_fence_after();
                 const unsigned long long bad = *(volatile unsigned long long*)&ctl->bad[item & 3u] & see;
-                const int slot = (int)blockIdx.x * 2 + (item ? 1 : 0);   // an item that is not the block's first is its last, or whole
+                const int slot = (int)blockIdx.x + (item ? P.blocks : 0);   // an item that is not the block's first is its last, or whole
                 float* po = P.part_o + (long long)slot * P.part_rows * HD + (t >> 2) * (4 * HD) + (t & 3) * 8;
                 T* dst = (T*)P.out + (sq.first + j) * P.out_row_stride + (cur.h * P.g + hh) * P.out_head_stride;
                 const float sc = whole ? 1.f / l : 1.f;
@@ -522,169 +514,176 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     if (tid == 0 && ctl->abort_flag && P.status) atomicExch(P.status, 1);
 }
 
-// Output rows whose keys several blocks went through: un-normalised partial outputs weighted by 2^(maximum - largest maximum).  The work is in units of four tile rows of an
-// item (of 32 columns each when `split`: where there are few units), a lane has four columns of one row.  A block takes `group` units at a time; one with up to four parts is one
-// warp's, one with more the whole block's (a long cache of few sequences is cut into up to 150 parts).  Where the parts are follows from the lengths alone
-// and is worked out before the attention is waited for.
-constexpr int kMergeWarps = 16, kMergeThreads = kMergeWarps * 32, kMergeFew = 4, kMergeDeep = 5;   // parts a warp has in flight
+// Output rows whose keys several blocks went through: un-normalised partial outputs weighted by 2^(maximum - largest maximum).  A unit is four tile rows of an
+// item, 32 columns of them when `split`, which is where there are few units; a lane has four columns of one row.  A warp takes a unit; those with more than ten
+// parts are gone through by whole blocks (a long cache of few sequences is cut into up to 150 parts).  Neighbouring units are in different blocks, so that a long
+// sequence among short ones has many blocks' help.  Where the parts are follows from the lengths alone and is worked out before the attention is waited for.
+// Bound by latency: launch, a round trip to L2 for five parts, the store.
+constexpr int kMergeWarps = 16, kMergeThreads = kMergeWarps * 32, kMergeDeep = 4 /* parts a warp has in flight */, kMergeFew = 3 * kMergeDeep;
 struct TreeUnit {
     int block0, n;        // first block with a part, parts
-    int row, rows;        // first tile row, rows
-    int b, h, j0;         // sequence, KV head, first (row, head of the group) of the unit within the sequence
-    int col0, cols;       // columns
+    int row, rows, col;   // first tile row, rows, first column
+    int first, h, j0;     // first row of the sequence, KV head, first (row, head of the group) of the unit within the sequence
     bool late;            // of block0 it is the second partial item
-    __device__ __forceinline__ int slot(int i) const { return (block0 + i) * 2 + (i == 0 && late ? 1 : 0); }
+    __device__ __forceinline__ int slot(int i, int blocks) const { return block0 + i + (i == 0 && late ? blocks : 0); }
 };
+
+__device__ __forceinline__ void tree_add(float4& o, float w, const float4& x) { o.x += w * x.x; o.y += w * x.y; o.z += w * x.z; o.w += w * x.w; }
+__device__ __forceinline__ void tree_scale(float4& o, float w) { o.x *= w; o.y *= w; o.z *= w; o.w *= w; }
+
+// What a lane has of a unit: a row, four columns of every group of 32.
+template <typename T, int HD>
+struct TreeMergeRow {
+    const float2* ml;
+    const float* o;    // (at most 1024 blocks of two parts of 128 rows of 128 columns: offsets within 32 bits)
+    __device__ __forceinline__ TreeMergeRow(const TreeParams& P, const TreeUnit& q, int my_row, int lane) {
+        ml = P.part_ml + q.row + my_row;
+        o = P.part_o + q.row * HD + (lane >> 3) * 32 + my_row * 8 + (lane & 1) * 4;
+    }
+    __device__ __forceinline__ void store(const TreeParams& P, const TreeUnit& q, int my_row, int lane, int c, const float4& v, float sum) const {
+        const float sc = 1.f / sum;
+        const int r = q.j0 + my_row, j = r / P.g, hh = r - j * P.g;
+        T* dst = (T*)P.out + (q.first + j) * P.out_row_stride + (q.h * P.g + hh) * P.out_head_stride + (lane >> 3) * 8 + (lane & 1) * 4;
+        if (my_row < q.rows) *reinterpret_cast<uint2*>(dst + c) = make_uint2(Half16<T>::pack(v.x * sc, v.y * sc), Half16<T>::pack(v.z * sc, v.w * sc));
+    }
+};
+
+// Adds parts i0, i0 + step, ... of a unit, up to five, to (maximum, sum, output).
+template <int HD>
+__device__ __forceinline__ void tree_gather(const TreeParams& P, const TreeUnit& q, const float2* ml0, const float* o0, int i0, int step, float& m, float& l, float4& o) {
+    float2 ml[kMergeDeep];
+    float4 x[kMergeDeep];
+#pragma unroll
+    for (int t = 0; t < kMergeDeep; ++t) {
+        const int i = i0 + t * step;
+        ml[t] = make_float2(-CUDART_INF_F, 0.f);
+        if (i < q.n) {
+            const int at = q.slot(i, P.blocks) * P.part_rows;
+            ml[t] = __ldcg(ml0 + at);
+            x[t] = __ldcg(reinterpret_cast<const float4*>(o0 + at * HD));
+        }
+    }
+    float mx = m;
+#pragma unroll
+    for (int t = 0; t < kMergeDeep; ++t) mx = fmaxf(mx, ml[t].x);
+    const float ref = mx == -CUDART_INF_F ? 0.f : mx, keep = exp2f(m - ref);
+    m = mx;
+    l *= keep;
+    tree_scale(o, keep);
+#pragma unroll
+    for (int t = 0; t < kMergeDeep; ++t)
+        if (i0 + t * step < q.n) {
+            const float f = exp2f(ml[t].x - ref);
+            l += f * ml[t].y;
+            tree_add(o, f, x[t]);
+        }
+}
 
 template <typename T, int HD>
 __global__ void __launch_bounds__(kMergeThreads, 2) tree_merge_kernel(const __grid_constant__ TreeParams P, int group, int split) {
     __shared__ TreeScan<kMergeWarps> scan;
+    __shared__ int unit0[kMergeThreads];   // first unit of every thread's first sequence
     __shared__ TreeUnit shared_unit[kMergeWarps];
     __shared__ float4 shared_o[kMergeWarps][32];
     __shared__ float2 shared_ml[kMergeWarps][32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, my_row = (lane >> 1) & 3, my_col = (lane >> 3) * 8 + (lane & 1) * 4;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, my_row = (lane >> 1) & 3;
+    // Rows of units are numbered by the (row, query head) pairs of a KV head in fours, those of a sequence beginning a new one.  (The host sees to it that
+    // the number of units stays within 32 bits.)
+    const auto first_unit = [&](int b) { return (int)((unsigned)(rows_begin(P.cu_rows, b, P.n_rows) * P.g + 3) / 4u) + b; };
+    const int per = TreeScan<kMergeWarps>::per(P);
+    unit0[threadIdx.x] = (int)threadIdx.x * per < P.n_seqs ? first_unit((int)threadIdx.x * per) : INT_MAX;
     scan.fill(P);
     __syncthreads();
     const long long total = scan.total();
-    const int sharers = tree_sharers(total, P.blocks);
-    // units are numbered by the rows of the whole call: (row, query head) pairs of a KV head in fours, those of a sequence beginning a new one; sequence b's begin at
-    // ceil(first row * g / 4) + b
-    const long long units = ((long long)P.n_rows * P.g + 3) / 4 + P.n_seqs, tasks = units * P.n_kv * split;
+    const int sharers = tree_sharers(total, P.blocks), cols = HD / split;
+    const unsigned tasks = ((unsigned)(P.n_rows * P.g + 3) / 4u + P.n_seqs) * P.n_kv * split;
     bool waited = false;
-    // (at most 1024 blocks of two parts of 128 rows of 128 columns: offsets within 32 bits)
-    const int o_lane = (lane >> 3) * 32 + my_row * 8 + (lane & 1) * 4;
-    const auto ml_of = [&](const TreeUnit& q, int i) { return __ldcg(P.part_ml + q.slot(i) * P.part_rows + q.row + my_row); };
-    const auto o_of = [&](const TreeUnit& q, int i, int c) {
-        return __ldcg(reinterpret_cast<const float4*>(P.part_o + (q.slot(i) * P.part_rows + q.row) * HD + c * 4 + o_lane));
-    };
-    const auto store = [&](const TreeUnit& q, int c, const float4& o, float sum) {
-        const int r = q.j0 + my_row, j = r / P.g, hh = r - j * P.g;
-        if (my_row >= q.rows) return;
-        T* dst = (T*)P.out + (rows_begin(P.cu_rows, q.b, P.n_rows) + j) * P.out_row_stride + (q.h * P.g + hh) * P.out_head_stride + c + my_col;
-        const float sc = 1.f / sum;
-        *reinterpret_cast<uint2*>(dst) = make_uint2(Half16<T>::pack(o.x * sc, o.y * sc), Half16<T>::pack(o.z * sc, o.w * sc));
-    };
-    const auto add = [](float4& o, float w, const float4& x) { o.x += w * x.x; o.y += w * x.y; o.z += w * x.z; o.w += w * x.w; };
-    for (long long p0 = (long long)blockIdx.x * group; p0 < tasks; p0 += (long long)gridDim.x * group) {
-        TreeUnit q;
-        q.n = 0;
-        const long long task = p0 + warp;
-        if (warp < group && task < tasks && total > 0) {
-            const int part = (int)(task % split);
-            const long long u = task / split;
-            q.h = (int)(u % P.n_kv);
-            const long long unit = u / P.n_kv;
-            // the last sequence that begins at or before the unit, by ballots
-            int lo = 0, n = P.n_seqs;
-            while (n > 1) {
-                const int step = (n + 31) / 32, at = lo + lane * step;
-                const bool begins = lane * step < n && ((long long)rows_begin(P.cu_rows, at, P.n_rows) * P.g + 3) / 4 + at <= unit;
-                const int k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, begins)));
-                n = min(step, n - k * step);
-                lo += k * step;
+    for (unsigned p0 = blockIdx.x; p0 < tasks; p0 += gridDim.x * group) {
+        if (warp < group) {
+            const unsigned task = p0 + warp * gridDim.x;
+            TreeUnit q;
+            q.n = 0;
+            if (task < tasks && total > 0) {
+                const unsigned u = task / split, unit_u = u / P.n_kv;
+                const int unit = (int)unit_u;
+                q.col = (int)(task - u * split) * cols;
+                q.h = (int)(u - unit_u * P.n_kv);
+                // the last sequence that begins at or before the unit, and the tiles before it
+                long long tile0 = 0;
+                int w = 0;
+                while (w < kMergeWarps - 1 && unit0[(w + 1) * 32] <= unit) tile0 += scan.warp_sum[w++];
+                const int t = w * 32 + max(0, 31 - __clz(__ballot_sync(0xffffffffu, unit0[w * 32 + lane] <= unit)));
+                tile0 += scan.before[t];
+                int b = t * per;
+                const int end = min(b + per, P.n_seqs) - 1;
+                while (b < end && first_unit(b + 1) <= unit) tile0 += tree_tiles(P, tree_seq(P, b++));
+                const TreeSeq s = tree_seq(P, b);
+                const int j0 = (unit - first_unit(b)) * 4;
+                if (j0 >= 0 && j0 < s.rows * P.g && s.tiles > 0) {
+                    q.first = s.first;
+                    q.j0 = j0;
+                    q.rows = min(4, s.rows * P.g - j0);
+                    const int c = j0 / kTreeTileRows;
+                    tile0 += (long long)(q.h * s.chunks + c) * s.tiles;
+                    q.block0 = tree_owner(total, tile0, sharers);
+                    q.n = tree_owner(total, tile0 + s.tiles - 1, sharers) - q.block0 + 1;
+                    q.row = j0 - c * kTreeTileRows;
+                    q.late = tree_share(total, q.block0, sharers) < tile0;
+                }
             }
-            const TreeSeq s = tree_seq(P, lo);
-            q.b = lo;
-            const long long j0 = (unit - (((long long)s.first * P.g + 3) / 4 + lo)) * 4;
-            if (j0 >= 0 && j0 < (long long)s.rows * P.g && s.tiles > 0) {
-                q.j0 = (int)j0;
-                q.rows = min(4, s.rows * P.g - q.j0);
-                const int c = q.j0 / kTreeTileRows;
-                const long long tile0 = scan.tiles_before(P, lo) + ((long long)q.h * s.chunks + c) * s.tiles;
-                q.block0 = tree_owner(total, tile0, sharers);
-                q.n = tree_owner(total, tile0 + s.tiles - 1, sharers) - q.block0 + 1;
-                q.row = q.j0 - c * kTreeTileRows;
-                q.late = tree_share(total, q.block0, sharers) < tile0;
-                q.cols = HD / split;
-                q.col0 = part * q.cols;
-            }
+            if (lane == 0) shared_unit[warp] = q;
         }
-        if (lane == 0) shared_unit[warp] = q;
-        __syncwarp();
         if (!waited) grid_dep_wait();   // the parts are there
         waited = true;
-        const TreeUnit& mine = shared_unit[warp];
-        if (q.n > 1 && q.n <= kMergeFew) {
-            float2 ml[kMergeFew];
-#pragma unroll
-            for (int i = 0; i < kMergeFew; ++i) ml[i] = i < mine.n ? ml_of(mine, i) : make_float2(-CUDART_INF_F, 0.f);
-            const float mx = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), ref = mx == -CUDART_INF_F ? 0.f : mx;
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < kMergeFew; ++i) {
-                ml[i].x = exp2f(ml[i].x - ref);
-                sum += ml[i].x * ml[i].y;
-            }
-#pragma unroll 2
-            for (int c = mine.col0; c < mine.col0 + mine.cols; c += 32) {
-                float4 x[kMergeFew], o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int i = 0; i < kMergeFew; ++i)
-                    if (i < mine.n) x[i] = o_of(mine, i, c);
-#pragma unroll
-                for (int i = 0; i < kMergeFew; ++i)
-                    if (i < mine.n) add(o, ml[i].x, x[i]);
-                store(mine, c, o, sum);
-            }
-        }
-        __syncthreads();
-        for (int k = 0; k < group; ++k) {
-            if (shared_unit[k].n <= kMergeFew) continue;   // the same for the whole block
-            const TreeUnit& w = shared_unit[k];
-            for (int c = w.col0; c < w.col0 + w.cols; c += 32) {
-                // a warp's parts: warp, warp + 16, ...
-                float m = -CUDART_INF_F, l = 0.f;
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                constexpr int DEEP = kMergeDeep;
+        __syncwarp();
+        bool many = false;
+        if (warp < group) {
+            const TreeUnit& q = shared_unit[warp];
+            many = q.n > kMergeFew;
+            if (q.n > 1 && !many) {
+                TreeMergeRow<T, HD> row(P, q, my_row, lane);
 #pragma unroll 1
-                for (int i0 = warp; i0 < w.n; i0 += DEEP * kMergeWarps) {
-                    float2 ml[DEEP];
-                    float4 x[DEEP];
-#pragma unroll
-                    for (int t = 0; t < DEEP; ++t) {
-                        const int i = i0 + t * kMergeWarps;
-                        ml[t] = make_float2(-CUDART_INF_F, 0.f);
-                        if (i < w.n) {
-                            ml[t] = ml_of(w, i);
-                            x[t] = o_of(w, i, c);
-                        }
-                    }
-                    float mx = m;
-#pragma unroll
-                    for (int t = 0; t < DEEP; ++t) mx = fmaxf(mx, ml[t].x);
-                    const float ref = mx == -CUDART_INF_F ? 0.f : mx, keep = exp2f(m - ref);
-                    l *= keep;
-                    o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
-#pragma unroll
-                    for (int t = 0; t < DEEP; ++t)
-                        if (i0 + t * kMergeWarps < w.n) {
-                            const float f = exp2f(ml[t].x - ref);
-                            l += f * ml[t].y;
-                            add(o, f, x[t]);
-                        }
-                    m = mx;
+                for (int c = q.col; c < q.col + cols; c += 32) {
+                    float m = -CUDART_INF_F, l = 0.f;
+                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+                    for (int i0 = 0; i0 < q.n; i0 += kMergeDeep) tree_gather<HD>(P, q, row.ml, row.o + c * 4, i0, 1, m, l, o);
+                    row.store(P, q, my_row, lane, c, o, l);
                 }
-                shared_o[warp][lane] = o;
-                shared_ml[warp][lane] = make_float2(m, l);
-                __syncthreads();
-                if (warp == 0) {
-                    float mx = -CUDART_INF_F, sum = 0.f;
-#pragma unroll
-                    for (int t = 0; t < kMergeWarps; ++t) mx = fmaxf(mx, shared_ml[t][lane].x);
-                    const float ref = mx == -CUDART_INF_F ? 0.f : mx;
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int t = 0; t < kMergeWarps; ++t) {
-                        const float f = exp2f(shared_ml[t][lane].x - ref);
-                        sum += f * shared_ml[t][lane].y;
-                        add(v, f, shared_o[t][lane]);
-                    }
-                    store(w, c, v, sum);
-                }
-                __syncthreads();
             }
         }
-        __syncthreads();   // shared_unit is read before the next units'
+        if (!__syncthreads_or(many)) continue;
+        // those with many parts, one after the other: as many columns at once as a unit has (in groups of 32), the parts shared out among the warps that remain for each
+        const int groups = cols / 32, step = kMergeWarps / groups;
+#pragma unroll 1
+        for (int k = 0; k < group; ++k) {
+            const TreeUnit& q = shared_unit[k];
+            if (q.n <= kMergeFew) continue;   // the same for the whole block
+            TreeMergeRow<T, HD> row(P, q, my_row, lane);
+            const int c = q.col + warp % groups * 32;
+            float m = -CUDART_INF_F, l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+            for (int i0 = warp / groups; i0 < q.n; i0 += kMergeDeep * step) tree_gather<HD>(P, q, row.ml, row.o + c * 4, i0, step, m, l, o);
+            shared_o[warp][lane] = o;
+            shared_ml[warp][lane] = make_float2(m, l);
+            __syncthreads();
+            if (warp < groups) {
+                float mx = -CUDART_INF_F, sum = 0.f;
+                for (int t = warp; t < kMergeWarps; t += groups) mx = fmaxf(mx, shared_ml[t][lane].x);
+                const float ref = mx == -CUDART_INF_F ? 0.f : mx;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                for (int t = warp; t < kMergeWarps; t += groups) {
+                    const float2 ml = shared_ml[t][lane];
+                    const float f = exp2f(ml.x - ref);
+                    sum += f * ml.y;
+                    tree_add(v, f, shared_o[t][lane]);
+                }
+                row.store(P, q, my_row, lane, c, v, sum);
+            }
+            __syncthreads();
+        }
     }
 }
 

@@ -5,57 +5,57 @@
 namespace sdv {
 
 constexpr int kVerifyThreads = 512, kVerifyWarps = kVerifyThreads / 32;
-constexpr int kVerifyTile = 512;             // vocabulary entries a warp sums up at a time: four groups of four a lane
+constexpr int kVerifyTile = 512;             // vocabulary entries a warp sums up at a time: sixteen a lane
 constexpr int kVerifyMaxCluster = 8;
 
-__device__ __forceinline__ double ld_cluster_f8(uint32_t addr) {
-    double v;
-    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr));
-    return v;
-}
+__device__ __forceinline__ void st_cluster_f8(uint32_t addr, double v) { asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory"); }
 
 // What the drawn token's distribution is made of.
 struct VerifyRest {
     const float *p, *q;      // target's row; rejected draft's row or null
     const int* out;          // tokens without a share (shared memory)
     int n_out, vocab;
-    bool wide_p, wide_q;     // rows start on 16-byte boundaries
+    bool wide;               // rows start on 16-byte boundaries
 };
 
-// Weights of entries at .. at + 3 (0 past the end) in 64 bits: the difference of two fp32 numbers is exact there.
-__device__ __forceinline__ void verify_weights(const VerifyRest& d, int at, double (&w)[4]) {
-    float p[4] = {0.f, 0.f, 0.f, 0.f}, q[4] = {0.f, 0.f, 0.f, 0.f};
-    if (at + 3 < d.vocab && d.wide_p) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(d.p + at));
-        p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w;
+// Sixteen entries of a tile: lane's four from each of four places `apart` entries apart (0 past the end), as the fp32 pairs whose differences are the shares: an entry without
+// a share is 0 - 0.  The difference of two fp32 numbers and their sum over a vocabulary are near enough exact in 64 bits.
+__device__ __forceinline__ void verify_load(const VerifyRest& d, int first, int apart, float (&p)[16], float (&q)[16]) {
+    if (first + 3 * apart + 3 < d.vocab && d.wide) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(d.p + first + k * apart));
+            p[4 * k] = v.x; p[4 * k + 1] = v.y; p[4 * k + 2] = v.z; p[4 * k + 3] = v.w;
+        }
+        if (d.q) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(d.q + first + k * apart));
+                q[4 * k] = v.x; q[4 * k + 1] = v.y; q[4 * k + 2] = v.z; q[4 * k + 3] = v.w;
+            }
+        }
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (at + j < d.vocab) p[j] = __ldcg(d.p + at + j);
+        for (int i = 0; i < 16; ++i) {
+            const int at = first + (i >> 2) * apart + (i & 3);
+            p[i] = at < d.vocab ? __ldcg(d.p + at) : 0.f;
+            q[i] = d.q && at < d.vocab ? __ldcg(d.q + at) : 0.f;
+        }
     }
-    if (d.q) {
-        if (at + 3 < d.vocab && d.wide_q) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(d.q + at));
-            q[0] = v.x; q[1] = v.y; q[2] = v.z; q[3] = v.w;
-        } else {
+    for (int n = 0; n < d.n_out; ++n) {
+        const int at = d.out[n] - first;
+        if ((unsigned)at < (unsigned)(3 * apart + 4)) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (at + j < d.vocab) q[j] = __ldcg(d.q + at + j);
+            for (int i = 0; i < 16; ++i)
+                if (at == (i >> 2) * apart + (i & 3)) p[i] = 0.f;
         }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const double x = (double)p[j] - (double)q[j];
-        w[j] = p[j] > 0.f && x > 0.0 ? x : 0.0;   // NaN has no share either
-    }
-    for (int i = 0; i < d.n_out; ++i) {
-        const unsigned j = (unsigned)(d.out[i] - at);
-        if (j < 4u) {
-            if (j == 0) w[0] = 0.0;
-            if (j == 1) w[1] = 0.0;
-            if (j == 2) w[2] = 0.0;
-            if (j == 3) w[3] = 0.0;
-        }
+    for (int i = 0; i < 16; ++i) {
+        if (!d.q) q[i] = 0.f;
+        const bool has = p[i] > 0.f && p[i] > q[i];   // NaN has none
+        p[i] = has ? p[i] : 0.f;
+        q[i] = has ? q[i] : 0.f;
     }
 }
 
@@ -63,13 +63,13 @@ __device__ __forceinline__ void verify_weights(const VerifyRest& d, int at, doub
 // remains, tile by tile in a fixed order; the blocks' sums meet through distributed shared memory, and the block whose share holds the drawn token reads that one
 // tile again.  Sums in 64 bits: a token's share may be 10^-9 of the whole, fp32 sums would draw its neighbour.  Bound by reading the row (and
 // the draft's) once, for few sequences by the chain of round trips: rows, tokens, shares, row, tile.
-__global__ void __launch_bounds__(kVerifyThreads) verify_sampled_kernel(const __grid_constant__ sdv_verify_args a, int tiles_per_block) {
+__global__ void __launch_bounds__(kVerifyThreads, 2) verify_sampled_kernel(const __grid_constant__ sdv_verify_args a, int tiles_per_block) {
     extern __shared__ double tile_sum[];   // [tiles_per_block]
     __shared__ int tok[SDV_TREE_ROWS], par[SDV_TREE_ROWS], out[SDV_TREE_ROWS], path[SDV_TREE_ROWS], child[SDV_TREE_ROWS];
     __shared__ float share[SDV_TREE_ROWS];
     __shared__ unsigned char again[SDV_TREE_ROWS];
     __shared__ int n_path, n_out, rejected_row;
-    __shared__ double total;
+    __shared__ double sums[2][kVerifyMaxCluster];   // of every block's share
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int CS = (int)cluster_size(), rank = (int)cluster_rank(), b = (int)blockIdx.x / CS;
     const int first = rows_begin(a.cu_rows, b, a.n_rows), all = rows_count(a.cu_rows, b, a.n_rows), T = min(all, SDV_TREE_ROWS);
@@ -85,6 +85,8 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_sampled_kernel(const __
         if (rank == 0 && tid == 0) a.accept_len[b] = -1;
         return;
     }
+    cluster_arrive_relaxed();   // waited for before anything is written to another block, which has started by then
+    const float draw = __ldg(a.uniforms + first);
     const int i = tid;
     float u = 0.f, q = 1.f;
     if (i < SDV_TREE_ROWS) {
@@ -170,19 +172,15 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_sampled_kernel(const __
     d.q = rejected_row >= 0 ? a.draft + (first + rejected_row) * a.draft_stride : nullptr;
     d.out = out;
     d.n_out = n_out;
-    d.wide_p = ((uintptr_t)d.p & 15) == 0;
-    d.wide_q = ((uintptr_t)d.q & 15) == 0;
+    d.wide = (((uintptr_t)d.p | (uintptr_t)d.q) & 15) == 0;
     const int tiles = (a.vocab + kVerifyTile - 1) / kVerifyTile, tile0 = rank * tiles_per_block, mine = max(0, min(tiles - tile0, tiles_per_block));
-    const float draw = __ldg(a.uniforms + first);
     for (int attempt = 0;; ++attempt) {
         for (int t = warp; t < mine; t += kVerifyWarps) {
+            float p[16], q[16];
+            verify_load(d, (tile0 + t) * kVerifyTile + lane * 4, 128, p, q);
             double sum = 0.0;
 #pragma unroll
-            for (int k = 0; k < kVerifyTile / 128; ++k) {
-                double w[4];
-                verify_weights(d, (tile0 + t) * kVerifyTile + k * 128 + lane * 4, w);
-                sum += (w[0] + w[1]) + (w[2] + w[3]);
-            }
+            for (int i = 0; i < 16; ++i) sum += d.q ? (double)p[i] - (double)q[i] : (double)p[i];
 #pragma unroll
             for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
             if (lane == 0) tile_sum[t] = sum;
@@ -193,105 +191,90 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_sampled_kernel(const __
             for (int t = lane; t < mine; t += 32) sum += tile_sum[t];
 #pragma unroll
             for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            if (lane == 0) total = sum;
+            if (attempt == 0) cluster_wait();
+            // to every block of the cluster; each attempt has a place of its own, so that nobody waits for the readers
+            if (lane < CS) st_cluster_f8(map_shared_rank(smem_u32(&sums[attempt][rank]), lane), sum);
             __syncwarp();
+        } else if (attempt == 0) {
+            cluster_wait();
         }
-        __syncthreads();
         cluster_sync();
         double before = 0.0, whole = 0.0;
-        int holder = -1;   // the first block behind which the cumulative sum exceeds the target, else the last one with a share
+        for (int k = 0; k < CS; ++k) whole += sums[attempt][k];
+        const double goal = (double)draw * whole;
+        int holder = -1;   // the first block behind which the cumulative sum exceeds the goal, else the last one with a share
         {
-            double sums[kVerifyMaxCluster];
-#pragma unroll
-            for (int k = 0; k < kVerifyMaxCluster; ++k) sums[k] = k < CS ? ld_cluster_f8(map_shared_rank(smem_u32(&total), k)) : 0.0;
-#pragma unroll
-            for (int k = 0; k < kVerifyMaxCluster; ++k) whole += sums[k];
-            const double goal = (double)draw * whole;
             double cum = 0.0;
             bool done = false;
-#pragma unroll
-            for (int k = 0; k < kVerifyMaxCluster; ++k) {
-                if (!done && sums[k] > 0.0) {
+            for (int k = 0; k < CS && !done; ++k) {
+                const double x = sums[attempt][k];
+                if (x > 0.0) {
                     holder = k;
                     before = cum;
-                    done = cum + sums[k] > goal;
+                    done = cum + x > goal;
                 }
-                cum += sums[k];
+                cum += x;
             }
         }
-        cluster_sync();   // everybody has read the sums: they may be overwritten, and blocks may leave
         if (!(whole > 0.0)) {
             if (attempt == 0 && (d.q || d.n_out)) {   // nothing is left: the target's distribution itself
                 d.q = nullptr;
                 d.n_out = 0;
+                __syncthreads();   // tile_sum has been read
                 continue;
             }
             if (rank == 0 && tid == 0) a.out_tokens[first + a_len] = -1;
             return;
         }
-        if (rank != holder) return;
-        const double goal = (double)draw * whole;
-        if (warp == 0) {
-            // tile: the same rule over this block's tiles
-            double cum = before, at_before = before;
-            int at = -1;
-            bool done = false;
-            for (int t0 = 0; t0 < mine && !done; t0 += 32) {
-                const double x = t0 + lane < mine ? tile_sum[t0 + lane] : 0.0;
-                double incl = x;
+        if (rank != holder || warp > 0) return;
+        // tile: the same rule over this block's tiles
+        double cum = before, at_before = before;
+        int at = -1;
+        bool done = false;
+        for (int t0 = 0; t0 < mine && !done; t0 += 32) {
+            const double x = t0 + lane < mine ? tile_sum[t0 + lane] : 0.0;
+            double incl = x;
 #pragma unroll
-                for (int off = 1; off < 32; off <<= 1) {
-                    const double v = __shfl_up_sync(0xffffffffu, incl, off);
-                    if (lane >= off) incl += v;
-                }
-                const unsigned some = __ballot_sync(0xffffffffu, x > 0.0), over = __ballot_sync(0xffffffffu, x > 0.0 && cum + incl > goal);
-                if (some) {
-                    const int l = over ? __ffs(over) - 1 : 31 - __clz(some);
-                    at = t0 + l;
-                    at_before = cum + __shfl_sync(0xffffffffu, incl - x, l);
-                    done = over != 0;
-                }
-                cum += __shfl_sync(0xffffffffu, incl, 31);
+            for (int off = 1; off < 32; off <<= 1) {
+                const double v = __shfl_up_sync(0xffffffffu, incl, off);
+                if (lane >= off) incl += v;
             }
-            // entry: again over the tile's, in order
-            int token = -1;
-            cum = at_before;
-            done = false;
-            double w[kVerifyTile / 128][4];
-#pragma unroll
-            for (int k = 0; k < kVerifyTile / 128; ++k) verify_weights(d, (tile0 + at) * kVerifyTile + k * 128 + lane * 4, w[k]);
-#pragma unroll
-            for (int k = 0; k < kVerifyTile / 128; ++k) {
-                if (done) continue;
-                double part[4];
-                part[0] = w[k][0];
-                part[1] = part[0] + w[k][1];
-                part[2] = part[1] + w[k][2];
-                part[3] = part[2] + w[k][3];
-                double incl = part[3];
-#pragma unroll
-                for (int off = 1; off < 32; off <<= 1) {
-                    const double v = __shfl_up_sync(0xffffffffu, incl, off);
-                    if (lane >= off) incl += v;
-                }
-                const double lead = cum + (incl - part[3]);
-                int hit = -1, some = -1;
-#pragma unroll
-                for (int j = 3; j >= 0; --j) {
-                    if (w[k][j] > 0.0 && lead + part[j] > goal) hit = j;
-                    if (w[k][3 - j] > 0.0) some = 3 - j;
-                }
-                const unsigned has = __ballot_sync(0xffffffffu, some >= 0), over = __ballot_sync(0xffffffffu, hit >= 0);
-                if (has) {
-                    const int l = over ? __ffs(over) - 1 : 31 - __clz(has);
-                    const int j = __shfl_sync(0xffffffffu, over ? hit : some, l);
-                    token = (tile0 + at) * kVerifyTile + k * 128 + l * 4 + j;
-                    done = over != 0;
-                }
-                cum += __shfl_sync(0xffffffffu, incl, 31);
+            const unsigned some = __ballot_sync(0xffffffffu, x > 0.0), over = __ballot_sync(0xffffffffu, x > 0.0 && cum + incl > goal);
+            if (some) {
+                const int l = over ? __ffs(over) - 1 : 31 - __clz(some);
+                at = t0 + l;
+                at_before = cum + __shfl_sync(0xffffffffu, incl - x, l);
+                done = over != 0;
             }
-            if (lane == 0) a.out_tokens[first + a_len] = token;
+            cum += __shfl_sync(0xffffffffu, incl, 31);
         }
+        // entry: again over the tile's, a lane sixteen in a row
+        float p[16], q[16];
+        const int from = (tile0 + at) * kVerifyTile + lane * 16;
+        verify_load(d, from, 4, p, q);
+        double part = 0.0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) part += (double)p[i] - (double)q[i];
+        double incl = part;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const double v = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += v;
+        }
+        double sum = at_before + (incl - part);
+        int hit = -1, some = -1;   // the first entry behind which the sum exceeds the goal, the last one with a share
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const double w = (double)p[i] - (double)q[i];
+            sum += w;
+            if (w > 0.0) {
+                some = i;
+                if (hit < 0 && sum > goal) hit = i;
+            }
+        }
+        const unsigned has = __ballot_sync(0xffffffffu, some >= 0), over = __ballot_sync(0xffffffffu, hit >= 0);
+        const int l = over ? __ffs(over) - 1 : has ? 31 - __clz(has) : 0;
+        if (lane == l) a.out_tokens[first + a_len] = from + (over ? hit : some);
         return;
     }
 }
