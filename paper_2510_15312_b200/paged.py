@@ -5,7 +5,6 @@ do not allow raises ValueError, what the library refuses SdvError.  Outputs not 
 work is queued on."""
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import math
 import struct
@@ -14,7 +13,7 @@ from typing import Optional
 import torch
 
 from . import binding
-from .binding import EINVAL, OK, SdvError
+from .binding import EINVAL, SdvError
 
 _vp, _i, _ll, _f = C.c_void_p, C.c_int, C.c_longlong, C.c_float
 
@@ -57,9 +56,18 @@ def _packer(structure):
 
 
 _pack_pages, _pack_slots, _pack_rope, _pack_attention, _pack_verify = (_packer(t) for t in (_Pages, _SlotsArgs, _RopeArgs, _AttentionArgs, _VerifyArgs))
-_i32 = torch.int32
+_i32, _f32, _f64, _u8 = torch.int32, torch.float32, torch.float64, torch.uint8
 _types = {torch.bfloat16: 0, torch.float16: 1}   # SDV_BF16, SDV_FP16
-_no_context = contextlib.nullcontext()
+
+
+def _empty_public(shape, strides, dtype):
+    return torch.empty_strided(shape, strides, dtype=dtype, device="cuda")
+
+
+try:   # the same in half the time (0.7 of 1.4 us), where torch has the function for it
+    from torch._C._dynamo.guards import _empty_strided_cuda as _empty
+except ImportError:
+    _empty = _empty_public
 _present = False                                 # whether a CUDA device has been seen
 
 
@@ -89,23 +97,35 @@ def _table(t, n: int, device: int):
 
 
 def _enter(stream):
-    """(current device, handle of the stream, context in which outputs are allocated)."""
-    global _present
+    """(current device, handle of the stream)."""
+    global _present, _empty
     if not _present:
         if not torch.cuda.is_available():
             raise SdvError(binding.ECUDA, "no CUDA device (there is no CPU fallback)")
+        try:   # not part of torch's documented interface: another version's may take other arguments
+            _empty((1,), (1,), _i32)
+        except Exception:
+            _empty = _empty_public
         _present = True
     device = torch.cuda.current_device()
     if stream is not None:
-        return device, stream.cuda_stream, torch.cuda.stream(stream)
+        return device, stream.cuda_stream
     try:   # the current stream's handle without a Stream object around it, where torch has the function for it
-        return device, torch._C._cuda_getCurrentRawStream(device), _no_context
+        return device, torch._C._cuda_getCurrentRawStream(device)
     except AttributeError:
-        return device, torch.cuda.current_stream().cuda_stream, _no_context
+        return device, torch.cuda.current_stream().cuda_stream
+
+
+def _vectors(stream, *lengths):
+    """Fresh int32 vectors for outputs, allocated on the stream that writes them."""
+    if stream is None:
+        return [_empty((n,), (1,), _i32) for n in lengths]
+    with torch.cuda.stream(stream):
+        return [_empty((n,), (1,), _i32) for n in lengths]
 
 
 def _check(rc: int, where: str):
-    if rc != OK:
+    if rc:
         raise SdvError(rc, where)
 
 
@@ -136,28 +156,36 @@ def _rows(t, device: int, what: str):
     return shape, (s0 if shape[0] > 1 else 0), (s1 if shape[1] > 1 else 0)
 
 
+def _fresh(stream, shape, dtype):
+    """A contiguous tensor [rows][heads][head dim] for an output."""
+    n, heads, dim = shape
+    if stream is None:
+        return _empty((n, heads, dim), (heads * dim, dim, 1), dtype)
+    with torch.cuda.stream(stream):
+        return _empty((n, heads, dim), (heads * dim, dim, 1), dtype)
+
+
 def paged_slots(kv_len, cu_rows, block_table, n_held, free_pages, free_state, page_size: int, n_rows: int, parent=None, out=None, stream=None):
     """Hands pages to the sequences that need more and gives every row its slot and position: (slots, positions, n_held, free_state) after the call;
     block_table [sequences][width] is updated in place.  free_state[0] is the first unused entry of free_pages; of the returned one, the second entry is the number of
     sequences that were refused for want of pages (their slots are -1).  out: the four tensors to write to."""
-    dev, s, alloc = _enter(stream)
-    n = kv_len.shape[0]
+    dev, s = _enter(stream)
+    n, = per_seq = kv_len.shape
+    per_row, listed, states = (n_rows,), free_pages.shape, free_state.shape
     table, width, table_stride = _table(block_table, n, dev)
-    if n_rows < 0 or free_state.dim() != 1 or free_state.shape[0] < 1 or free_pages.dim() != 1:
+    if n_rows < 0 or len(listed) != 1 or len(states) != 1 or states[0] < 1:
         raise ValueError("paged_slots: n_rows >= 0, a list of free pages and a free_state of at least one entry expected")
-    per_row, per_seq = (n_rows,), (n,)
     if out is None:
-        device = kv_len.device
-        with alloc:
-            out = (torch.empty(n_rows, dtype=_i32, device=device), torch.empty(n_rows, dtype=_i32, device=device), torch.empty(n, dtype=_i32, device=device),
-                   torch.empty(2, dtype=_i32, device=device))
-    slots, positions, held, free = out
+        out = slots, positions, held, free = _vectors(stream, n_rows, n_rows, n, 2)
+        to = (slots.data_ptr(), positions.data_ptr(), held.data_ptr(), free.data_ptr())
+    else:
+        slots, positions, held, free = out
+        to = (_index(slots, per_row, dev, "slots"), _index(positions, per_row, dev, "positions"), _index(held, per_seq, dev, "n_held (out)"), _index(free, (2,), dev, "free_state (out)"))
     a = _pack_slots(_index(kv_len, per_seq, dev, "kv_len"), _index(cu_rows, (n + 1,), dev, "cu_rows"), 0 if parent is None else _index(parent, per_row, dev, "parent"),
-                    _index(n_held, per_seq, dev, "n_held"), _index(free_pages, free_pages.shape, dev, "free_pages"), _index(free_state, free_state.shape, dev, "free_state"), table,
-                    _index(slots, per_row, dev, "slots"), _index(positions, per_row, dev, "positions"), _index(held, per_seq, dev, "n_held (out)"),
-                    _index(free, (2,), dev, "free_state (out)"), table_stride, n, n_rows, page_size, width, free_pages.shape[0])
+                    _index(n_held, per_seq, dev, "n_held"), _index(free_pages, listed, dev, "free_pages"), _index(free_state, states, dev, "free_state"), table, *to, table_stride, n, n_rows,
+                    page_size, width, listed[0])
     _check(binding.lib().sdv_paged_slots(a, s), "sdv_paged_slots")
-    return out
+    return slots, positions, held, free
 
 
 def rope_frequencies(rot_dim: int, theta: float = 1.0e4, scaling: Optional[str] = None, factor: float = 1.0, original_positions: int = 8192, low: float = 1.0, high: float = 4.0,
@@ -195,10 +223,9 @@ def rope_append(positions, frequencies, q=None, k=None, v=None, k_pages=None, v_
     """Rotates q [rows][query heads][head dim] and k [rows][KV heads][head dim] by positions [rows] (int32) times frequencies [rot_dim / 2] (float64); k and v go to their
     slots of the pages, a row whose slot is outside the pool is not written.  q, or k, v, the pages and slots, may be left out.  Returns the rotated q (q_out; may be q
     itself), None without q."""
-    dev, s, alloc = _enter(stream)
-    n = positions.shape[0]
-    per_row = (n,)
-    if frequencies.dtype is not torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous() or frequencies.get_device() != dev:
+    dev, s = _enter(stream)
+    n, = per_row = positions.shape
+    if frequencies.dtype is not _f64 or frequencies.dim() != 1 or not frequencies.is_contiguous() or frequencies.get_device() != dev:
         raise ValueError("frequencies: contiguous float64 [rot_dim / 2] on the current device expected")
     if (q is None and k is None) or (k is None) != (v is None):
         raise ValueError("rope_append: q, or k and v, expected")
@@ -220,11 +247,11 @@ def rope_append(positions, frequencies, q=None, k=None, v=None, k_pages=None, v_
             raise ValueError("q: a row for every position, with the head dim and type of k, expected")
         dtype, heads, dim = _dtype(q, "q"), shape[1], shape[2]
         if q_out is None:
-            with alloc:
-                q_out = torch.empty_like(q)
-        out_shape, out_row, out_head = _rows(q_out, dev, "q_out")
-        if out_shape != shape or q_out.dtype is not q.dtype:
-            raise ValueError("q_out: shape and type of q expected")
+            q_out, out_row, out_head = _fresh(stream, shape, q.dtype), heads * dim, dim
+        else:
+            out_shape, out_row, out_head = _rows(q_out, dev, "q_out")
+            if out_shape != shape or q_out.dtype is not q.dtype:
+                raise ValueError("q_out: shape and type of q expected")
         q_ptr, out_ptr = q.data_ptr(), q_out.data_ptr()
     half = frequencies.shape[0]
     a = _pack_rope(q_ptr, k_ptr, v_ptr, out_ptr, _index(positions, per_row, dev, "positions"), slot_ptr, frequencies.data_ptr(), q_row, q_head, out_row, out_head, k_row, k_head,
@@ -240,33 +267,43 @@ def tree_attention_workspace(n_seqs: int, head_dim: int):
     n = binding.lib().sdv_tree_attention_workspace_bytes(n_seqs, head_dim)
     if n == 0:
         raise SdvError(EINVAL, "sdv_tree_attention_workspace_bytes")
-    return torch.empty(n, dtype=torch.uint8, device="cuda")
+    return torch.empty(n, dtype=_u8, device="cuda")
 
 
 def tree_attention(q, k_pages, v_pages, block_table, kv_len, cu_rows, parent=None, scale: Optional[float] = None, out=None, workspace=None, status=None, stream=None):
     """Every row of q [rows][query heads][head dim] attends to the kv_len[b] committed tokens of its sequence and to the rows on its own path through
     the draft tree, whose keys and values were appended before.  scale: 1 / sqrt(head dim) unless given.  out: like q; rows of no sequence are left as they were.  workspace: see
     tree_attention_workspace; without one torch allocates it for the call.  status: int32 [1], set to 1 when a wait inside the kernel ran out."""
-    dev, s, alloc = _enter(stream)
+    dev, s = _enter(stream)
     pages = _pool(k_pages, v_pages, dev)
     shape, q_row, q_head = _rows(q, dev, "q")
     n, heads, dim = shape
-    if q.dtype is not k_pages.dtype or dim != pages[6]:
+    dtype = q.dtype
+    if dtype is not k_pages.dtype or dim != pages[6]:
         raise ValueError("q: type and head dim of the pages expected")
-    seqs = kv_len.shape[0]
+    seqs, = per_seq = kv_len.shape
     table, width, table_stride = _table(block_table, seqs, dev)
     lib = binding.lib()
-    with alloc:
-        if out is None:
-            out = torch.empty_like(q)
-        if workspace is None:
-            workspace = torch.empty(lib.sdv_tree_attention_workspace_bytes(seqs, dim), dtype=torch.uint8, device=q.device)
-    out_shape, out_row, out_head = _rows(out, dev, "out")
-    if out_shape != shape or out.dtype is not q.dtype or workspace.get_device() != dev or not workspace.is_contiguous():
-        raise ValueError("out: shape and type of q, workspace: contiguous memory of the current device expected")
-    a = _pack_attention(q.data_ptr(), out.data_ptr(), table, _index(kv_len, (seqs,), dev, "kv_len"), _index(cu_rows, (seqs + 1,), dev, "cu_rows"),
+    if out is None:
+        out, out_row, out_head = _fresh(stream, shape, dtype), heads * dim, dim
+    else:
+        out_shape, out_row, out_head = _rows(out, dev, "out")
+        if out_shape != shape or out.dtype is not dtype:
+            raise ValueError("out: shape and type of q expected")
+    if workspace is None:
+        size = lib.sdv_tree_attention_workspace_bytes(seqs, dim)
+        if stream is None:
+            workspace = _empty((size,), (1,), _u8)
+        else:
+            with torch.cuda.stream(stream):
+                workspace = _empty((size,), (1,), _u8)
+    else:
+        size = workspace.numel() * workspace.element_size()
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace: contiguous memory of the current device expected")
+    a = _pack_attention(q.data_ptr(), out.data_ptr(), table, _index(kv_len, per_seq, dev, "kv_len"), _index(cu_rows, (seqs + 1,), dev, "cu_rows"),
                         0 if parent is None else _index(parent, (n,), dev, "parent"), workspace.data_ptr(), 0 if status is None else _index(status, (1,), dev, "status"),
-                        workspace.numel() * workspace.element_size(), q_row, q_head, out_row, out_head, table_stride, seqs, n, heads, width, dim ** -0.5 if scale is None else scale)
+                        size, q_row, q_head, out_row, out_head, table_stride, seqs, n, heads, width, dim ** -0.5 if scale is None else scale)
     if n and seqs:
         _check(lib.sdv_tree_attention(a, _pack_pages(*pages), s), "sdv_tree_attention")
     return out
@@ -274,7 +311,7 @@ def tree_attention(q, k_pages, v_pages, block_table, kv_len, cu_rows, parent=Non
 
 def _probs(t, n: int, vocab: int, device: int, what: str):
     """(address, distance of rows) of float32 [rows][vocab]."""
-    if t.dtype is not torch.float32 or t.get_device() != device or t.shape != (n, vocab):
+    if t.dtype is not _f32 or t.get_device() != device or t.shape != (n, vocab):
         raise ValueError(f"{what}: float32 [rows][vocab] on the current device expected")
     row, column = t.stride()
     if column != 1 and vocab > 1:
@@ -286,8 +323,10 @@ def verify_sampled(target_probs, tokens, cu_rows, uniforms, draft_probs=None, pa
     """Accepts drafted tokens against the target's probabilities [rows][vocab] (float32) with the uniform random numbers uniforms [rows] and draws one
     token behind the accepted ones: (accept_len [sequences], tokens [rows], rows [rows], slots [rows] or None).  draft_probs [rows][vocab]: what each draft of a chain was sampled from; without, drafts
     count as certain (retrieved), and parent may make them trees.  slots: every row's slot, for the slots that accepted rows move to.  out: the tensors to write to."""
-    dev, s, alloc = _enter(stream)
-    n, seqs = tokens.shape[0], cu_rows.shape[0] - 1
+    dev, s = _enter(stream)
+    n, = per_row = tokens.shape
+    edges, = bounds = cu_rows.shape
+    seqs = edges - 1
     if target_probs.dim() != 2 or seqs < 0:
         raise ValueError("verify_sampled: target_probs [rows][vocab] and cu_rows [sequences + 1] expected")
     vocab = target_probs.shape[1]
@@ -295,19 +334,20 @@ def verify_sampled(target_probs, tokens, cu_rows, uniforms, draft_probs=None, pa
     draft, draft_stride = (0, 0) if draft_probs is None else _probs(draft_probs, n, vocab, dev, "draft_probs")
     if draft_probs is not None and parent is not None:
         raise ValueError("verify_sampled: drafts with probabilities are chains")
-    per_row = (n,)
-    if uniforms.dtype is not torch.float32 or uniforms.shape != per_row or not uniforms.is_contiguous() or uniforms.get_device() != dev:
+    if uniforms.dtype is not _f32 or uniforms.shape != per_row or not uniforms.is_contiguous() or uniforms.get_device() != dev:
         raise ValueError("uniforms: contiguous float32 [rows] on the current device expected")
     if out is None:
-        device = tokens.device
-        with alloc:
-            out = (torch.empty(seqs, dtype=_i32, device=device), torch.empty(n, dtype=_i32, device=device), torch.empty(n, dtype=_i32, device=device),
-                   None if slots is None else torch.empty(n, dtype=_i32, device=device))
-    accept, out_tokens, out_rows, out_slots = out
-    a = _pack_verify(target, draft, _index(tokens, per_row, dev, "tokens"), _index(cu_rows, (seqs + 1,), dev, "cu_rows"), 0 if parent is None else _index(parent, per_row, dev, "parent"),
-                     0 if slots is None else _index(slots, per_row, dev, "slots"), uniforms.data_ptr(), _index(accept, (seqs,), dev, "accept_len"),
-                     _index(out_tokens, per_row, dev, "tokens (out)"), _index(out_rows, per_row, dev, "rows (out)"), 0 if slots is None else _index(out_slots, per_row, dev, "slots (out)"),
-                     target_stride, draft_stride, seqs, n, vocab)
+        if slots is None:
+            (accept, out_tokens, out_rows), out_slots = _vectors(stream, seqs, n, n), None
+        else:
+            accept, out_tokens, out_rows, out_slots = _vectors(stream, seqs, n, n, n)
+        to = (accept.data_ptr(), out_tokens.data_ptr(), out_rows.data_ptr(), 0 if slots is None else out_slots.data_ptr())
+    else:
+        accept, out_tokens, out_rows, out_slots = out
+        to = (_index(accept, (seqs,), dev, "accept_len"), _index(out_tokens, per_row, dev, "tokens (out)"), _index(out_rows, per_row, dev, "rows (out)"),
+              0 if slots is None else _index(out_slots, per_row, dev, "slots (out)"))
+    a = _pack_verify(target, draft, _index(tokens, per_row, dev, "tokens"), _index(cu_rows, bounds, dev, "cu_rows"), 0 if parent is None else _index(parent, per_row, dev, "parent"),
+                     0 if slots is None else _index(slots, per_row, dev, "slots"), uniforms.data_ptr(), *to, target_stride, draft_stride, seqs, n, vocab)
     if n and seqs:
         _check(binding.lib().sdv_verify_sampled(a, s), "sdv_verify_sampled")
-    return out
+    return accept, out_tokens, out_rows, out_slots
