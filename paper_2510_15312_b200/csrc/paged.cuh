@@ -175,7 +175,7 @@ union Elements {
 // to 0.03 rad), then all heads of q, k and v in units of 2 W elements, W on either side of the pairs.  A unit is read whole before it is written, so q may be turned in place.
 // Bound by memory for prompts, by latency for the rows of a step.
 template <typename T, bool INTERLEAVED, int W>
-__global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_constant__ sdv_rope_args a, const __grid_constant__ sdv_pages pages, int tokens) {
+__global__ void __launch_bounds__(kRopeThreads, 8) rope_append_kernel(const __grid_constant__ sdv_rope_args a, const __grid_constant__ sdv_pages pages, int tokens) {
     extern __shared__ float2 turn[];   // [token][pair] cosine, sine
     const int half = a.rot_dim / 2, t0 = (int)blockIdx.x * tokens, n = min(tokens, a.n_rows - t0);
     for (int i = threadIdx.x; i < n * half; i += kRopeThreads) {

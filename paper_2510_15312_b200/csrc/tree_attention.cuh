@@ -17,8 +17,8 @@ struct TreeShape {
     static constexpr int kAtoms = HD / 64;                        // 64-column swizzled slabs of a row
     static constexpr int kQBytes = kTreeTileRows * HD * 2;
     static constexpr int kSlotBytes = kTreeKeys * HD * 2;         // keys or values of a tile
-    static constexpr int kSlots = HD == 128 ? 5 : 12;
-    static constexpr int kCtlBytes = 1024;
+    static constexpr int kSlots = HD == 128 ? 5 : 11;
+    static constexpr int kCtlBytes = HD == 128 ? 1024 : 2048;
     static constexpr int kSmemBytes = kQBytes + kSlots * kSlotBytes + kCtlBytes;   // two blocks an SM: at most 113 KB each
     static_assert(kSmemBytes <= 113 * 1024, "two blocks per SM");
 };
@@ -40,37 +40,43 @@ struct TreeParams : TreeLists {
 // Tiles of all sequences, summed up by a block: thread t has the sequences [t * per, (t + 1) * per).
 template <int WARPS>
 struct TreeScan {
-    long long warp_sum[WARPS], before[WARPS * 32];   // before: within its warp
+    int warp_sum[WARPS], before[WARPS * 32];   // before: within its warp
     __device__ __forceinline__ static int per(const TreeLists& P) { return (P.n_seqs + WARPS * 32 - 1) / (WARPS * 32); }
     __device__ __forceinline__ void fill(const TreeLists& P) {   // all threads; a barrier follows
         const int tid = threadIdx.x, lane = tid & 31, n = per(P), b0 = min(tid * n, P.n_seqs), b1 = min(b0 + n, P.n_seqs);
-        long long sum = 0;
+        int sum = 0;
         for (int b = b0; b < b1; ++b) sum += tree_tiles(P, tree_seq(P, b));
-        long long incl = sum;
+        int incl = sum;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, incl, off);
+            const int v = __shfl_up_sync(0xffffffffu, incl, off);
             if (lane >= off) incl += v;
         }
         before[tid] = incl - sum;
         if (lane == 31) warp_sum[tid >> 5] = incl;
     }
-    __device__ __forceinline__ long long total() const {
-        long long t = 0;
+    __device__ __forceinline__ int total() const {
+        int t = 0;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) t += warp_sum[w];
         return t;
     }
     // The sequence that has tile `tile` (below the total), and how far into it; whole warps.
-    __device__ __forceinline__ int find_tile(const TreeLists& P, long long& tile) const {
+    __device__ __forceinline__ int find_tile(const TreeLists& P, int& tile, TreeSeq& s) const {
         const int lane = threadIdx.x & 31;
         int w = 0;
-        while (w < WARPS - 1 && tile >= warp_sum[w]) tile -= warp_sum[w++];
+#pragma unroll
+        for (int k = 0; k < WARPS - 1; ++k)
+            if (w == k && tile >= warp_sum[k]) {
+                tile -= warp_sum[k];
+                ++w;
+            }
         const int t = w * 32 + 31 - __clz(__ballot_sync(0xffffffffu, before[w * 32 + lane] <= tile));   // the last thread that begins at or before it
         tile -= before[t];
         int b = t * per(P);
         for (;; ++b) {
-            const long long n = tree_tiles(P, tree_seq(P, b));
+            s = tree_seq(P, b);
+            const int n = tree_tiles(P, s);
             if (tile < n || b + 1 >= P.n_seqs) return b;
             tile -= n;
         }
@@ -164,10 +170,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         unsigned long long bad[4];     // rows of the tree with values that are not finite, by item (modulo 4)
         uint32_t tmem_base;
         int abort_flag;
+        TreeScan<kTreeThreads / 32> scan;
     };
-    typedef TreeScan<kTreeThreads / 32> Scan;
-    Scan& scan = *reinterpret_cast<Scan*>(Qs);   // before there are queries
-    static_assert(sizeof(Scan) <= S::kQBytes, "sums over the sequences");
     Ctl* ctl = reinterpret_cast<Ctl*>(ring + S::kSlots * S::kSlotBytes);
     static_assert(sizeof(Ctl) <= S::kCtlBytes, "control block");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
@@ -189,29 +193,31 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     }
     if (warp == 5) tmem_alloc(&ctl->tmem_base, 256);   // S0 | S1, 64 columns each | O, HD columns
     if (warp == 4 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &map_v : &map_k) : "memory");
-    scan.fill(P);
+    ctl->scan.fill(P);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctl->tmem_base;
     grid_dep_launch();
-    const long long total = scan.total();
-    const int sharers = tree_sharers(total, P.blocks);
-    const long long my0 = tree_share(total, (int)blockIdx.x, sharers), my1 = tree_share(total, (int)blockIdx.x + 1, sharers);
     TreeCursor cur;
     {
-        long long offset = my0;
-        const int b0 = my0 < my1 ? scan.find_tile(P, offset) : 0;
-        cur.start(P, b0, offset, my1 - my0);
+        const TreeCut cut(ctl->scan.total(), P.blocks);
+        int offset = cut.begin((int)blockIdx.x);
+        const int n = cut.begin((int)blockIdx.x + 1) - offset;
+        cur.left = 0;
+        if (n > 0) {
+            TreeSeq s;
+            const int b = ctl->scan.find_tile(P, offset, s);
+            cur.start(P, b, s, offset, n);
+        }
     }
-    __syncthreads();   // the queries take the sums' place
 
     if (warp == 4) {
         // ---- copies: K0 V0 K1 V1 ... through the ring
         const int box_keys = min(P.page_size, kTreeKeys), boxes = kTreeKeys / box_keys;   // per slab
         const int my_box = lane % boxes, my_atom = lane / boxes;
         uint32_t s = 0, par = 0;
-        long long issued = 0;
+        int issued = 0;
         bool ok = true;
         const auto page_of = [&](const TreeCursor& c, int tile) {   // page of this lane's box of a tile
             const int key = tile * kTreeKeys + my_box * box_keys;
@@ -519,7 +525,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
 // parts are gone through by whole blocks (a long cache of few sequences is cut into up to 150 parts).  Neighbouring units are in different blocks, so that a long
 // sequence among short ones has many blocks' help.  Where the parts are follows from the lengths alone and is worked out before the attention is waited for.
 // Bound by latency: launch, a round trip to L2 for five parts, the store.
-constexpr int kMergeWarps = 16, kMergeThreads = kMergeWarps * 32, kMergeDeep = 4 /* parts a warp has in flight */, kMergeFew = 3 * kMergeDeep;
+constexpr int kMergeWarps = 8, kMergeThreads = kMergeWarps * 32, kMergeDeep = 5 /* parts a warp has in flight */, kMergeFew = 12;
 struct TreeUnit {
     int block0, n;        // first block with a part, parts
     int row, rows, col;   // first tile row, rows, first column
@@ -580,7 +586,7 @@ __device__ __forceinline__ void tree_gather(const TreeParams& P, const TreeUnit&
 }
 
 template <typename T, int HD>
-__global__ void __launch_bounds__(kMergeThreads, 2) tree_merge_kernel(const __grid_constant__ TreeParams P, int group, int split) {
+__global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __grid_constant__ TreeParams P, int group, int split) {
     __shared__ TreeScan<kMergeWarps> scan;
     __shared__ int unit0[kMergeThreads];   // first unit of every thread's first sequence
     __shared__ TreeUnit shared_unit[kMergeWarps];
@@ -594,8 +600,8 @@ __global__ void __launch_bounds__(kMergeThreads, 2) tree_merge_kernel(const __gr
     unit0[threadIdx.x] = (int)threadIdx.x * per < P.n_seqs ? first_unit((int)threadIdx.x * per) : INT_MAX;
     scan.fill(P);
     __syncthreads();
-    const long long total = scan.total();
-    const int sharers = tree_sharers(total, P.blocks), cols = HD / split;
+    const int total = scan.total(), cols = HD / split;
+    const TreeCut cut(total, P.blocks);
     const unsigned tasks = ((unsigned)(P.n_rows * P.g + 3) / 4u + P.n_seqs) * P.n_kv * split;
     bool waited = false;
     for (unsigned p0 = blockIdx.x; p0 < tasks; p0 += gridDim.x * group) {
@@ -609,7 +615,7 @@ __global__ void __launch_bounds__(kMergeThreads, 2) tree_merge_kernel(const __gr
                 q.col = (int)(task - u * split) * cols;
                 q.h = (int)(u - unit_u * P.n_kv);
                 // the last sequence that begins at or before the unit, and the tiles before it
-                long long tile0 = 0;
+                int tile0 = 0;
                 int w = 0;
                 while (w < kMergeWarps - 1 && unit0[(w + 1) * 32] <= unit) tile0 += scan.warp_sum[w++];
                 const int t = w * 32 + max(0, 31 - __clz(__ballot_sync(0xffffffffu, unit0[w * 32 + lane] <= unit)));
@@ -624,11 +630,11 @@ __global__ void __launch_bounds__(kMergeThreads, 2) tree_merge_kernel(const __gr
                     q.j0 = j0;
                     q.rows = min(4, s.rows * P.g - j0);
                     const int c = j0 / kTreeTileRows;
-                    tile0 += (long long)(q.h * s.chunks + c) * s.tiles;
-                    q.block0 = tree_owner(total, tile0, sharers);
-                    q.n = tree_owner(total, tile0 + s.tiles - 1, sharers) - q.block0 + 1;
+                    tile0 += (q.h * s.chunks + c) * s.tiles;
+                    q.block0 = cut.owner(tile0);
+                    q.n = cut.owner(tile0 + s.tiles - 1) - q.block0 + 1;
                     q.row = j0 - c * kTreeTileRows;
-                    q.late = tree_share(total, q.block0, sharers) < tile0;
+                    q.late = cut.begin(q.block0) < tile0;
                 }
             }
             if (lane == 0) shared_unit[warp] = q;
@@ -643,12 +649,36 @@ __global__ void __launch_bounds__(kMergeThreads, 2) tree_merge_kernel(const __gr
             if (q.n > 1 && !many) {
                 TreeMergeRow<T, HD> row(P, q, my_row, lane);
 #pragma unroll 1
-                for (int c = q.col; c < q.col + cols; c += 32) {
+                for (int c = q.col; c < q.col + cols; c += 64) {   // two groups of 32 columns (split: one)
+                    const bool wide = cols > 32;
                     float m = -CUDART_INF_F, l = 0.f;
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                    float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll 1
-                    for (int i0 = 0; i0 < q.n; i0 += kMergeDeep) tree_gather<HD>(P, q, row.ml, row.o + c * 4, i0, 1, m, l, o);
-                    row.store(P, q, my_row, lane, c, o, l);
+                    for (int i = 0; i < q.n; i += 2) {   // two parts at a time
+                        const int at = q.slot(i, P.blocks) * P.part_rows, next = q.slot(i + 1, P.blocks) * P.part_rows;
+                        const bool two = i + 1 < q.n;
+                        const float2 a = __ldcg(row.ml + at), b = two ? __ldcg(row.ml + next) : make_float2(-CUDART_INF_F, 0.f);
+                        float4 x[2], y[2];
+#pragma unroll
+                        for (int g = 0; g < 2; ++g)
+                            if (g == 0 || wide) {
+                                x[g] = __ldcg(reinterpret_cast<const float4*>(row.o + at * HD + (c + g * 32) * 4));
+                                if (two) y[g] = __ldcg(reinterpret_cast<const float4*>(row.o + next * HD + (c + g * 32) * 4));
+                            }
+                        const float mx = fmaxf(m, fmaxf(a.x, b.x)), ref = mx == -CUDART_INF_F ? 0.f : mx, keep = exp2f(m - ref), fa = exp2f(a.x - ref), fb = exp2f(b.x - ref);
+                        m = mx;
+                        l = l * keep + fa * a.y + fb * b.y;
+#pragma unroll
+                        for (int g = 0; g < 2; ++g)
+                            if (g == 0 || wide) {
+                                tree_scale(o[g], keep);
+                                tree_add(o[g], fa, x[g]);
+                                if (two) tree_add(o[g], fb, y[g]);
+                            }
+                    }
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+                        if (g == 0 || wide) row.store(P, q, my_row, lane, c + g * 32, o[g], l);
                 }
             }
         }

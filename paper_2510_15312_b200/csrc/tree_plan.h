@@ -51,30 +51,40 @@ SDV_HD TreeSeq tree_seq(const TreeLists& P, int b) {
     s.tiles = s.rows ? (s.keys + kTreeKeys - 1) / kTreeKeys : 0;
     return s;
 }
-SDV_HD long long tree_tiles(const TreeLists& P, const TreeSeq& s) { return (long long)s.tiles * s.chunks * P.n_kv; }
+SDV_HD int tree_tiles(const TreeLists& P, const TreeSeq& s) { return s.tiles * s.chunks * P.n_kv; }
 
-// The tiles of all sequences, KV heads and row chunks in a row are cut into equal shares, one a block.
-SDV_HD int tree_sharers(long long total, int blocks) { return (int)min(total, (long long)blocks); }   // with one tile at least
-SDV_HD long long tree_share(long long total, int block, int sharers) { return block >= sharers ? total : total * block / sharers; }
-SDV_HD int tree_owner(long long total, long long tile, int sharers) { return (int)(((tile + 1) * sharers - 1) / total); }
+// The tiles of all sequences, KV heads and row chunks in a row are cut into shares, one a block: the first blocks have one more than the last.  (The host refuses calls
+// that could have 2^31 tiles.)
+struct TreeCut {
+    int base, more;        // tiles of the last blocks, blocks with one more
+    SDV_HD TreeCut(int total, int blocks) {
+        base = (int)((unsigned)total / (unsigned)blocks);
+        more = total - base * blocks;
+    }
+    SDV_HD int begin(int block) const { return block * base + min(block, more); }
+    SDV_HD int owner(int tile) const {
+        const int split = more * (base + 1);   // tiles of the blocks with one more
+        return tile < split ? (int)((unsigned)tile / (unsigned)(base + 1)) : more + (int)((unsigned)(tile - split) / (unsigned)base);
+    }
+};
 
 // Cursor over a block's tiles: sequence, KV head, row chunk, key tile.
 struct TreeCursor {
-    long long left;                    // tiles of the block still to do, this one included
+    int left;                          // tiles of the block still to do, this one included
     int b, h, c, tile;
     TreeSeq s;
-    SDV_HD void start(const TreeLists& P, int b0, long long offset, long long n) {
+    // n tiles from the offset-th of sequence b0 on (which has more than that)
+    SDV_HD void start(const TreeLists& P, int b0, const TreeSeq& seq, int offset, int n) {
         left = n;
         b = b0;
-        if (n <= 0) return;
-        s = tree_seq(P, b);
-        tile = (int)(offset % s.tiles);
-        const long long item = offset / s.tiles;
-        c = (int)(item % s.chunks);
-        h = (int)(item / s.chunks);
+        s = seq;
+        const int item = (int)((unsigned)offset / (unsigned)s.tiles);
+        tile = offset - item * s.tiles;
+        h = s.chunks == 1 ? item : (int)((unsigned)item / (unsigned)s.chunks);
+        c = item - h * s.chunks;
     }
     // Tiles of the present item that belong to this block, from the present one on.
-    SDV_HD int run() const { return (int)min(left, (long long)(s.tiles - tile)); }
+    SDV_HD int run() const { return min(left, s.tiles - tile); }
     SDV_HD void skip(const TreeLists& P, int n) {   // n = run()
         left -= n;
         if (left <= 0) return;

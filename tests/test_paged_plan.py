@@ -24,22 +24,22 @@ static int check(const TreeLists& P, int blocks) {
         if (s.first < 0 || s.rows < 0 || s.first + s.rows > P.n_rows || s.rows > SDV_TREE_ROWS) return 1;
         if (s.length < 0 || s.keys < s.length || (long long)s.keys > (long long)P.table_width * P.page_size) return 2;
         if (s.keys - s.length > s.rows || (s.tiles > 0 && (s.tiles - 1) * kTreeKeys >= s.keys)) return 3;
-        before.push_back(before.back() + tree_tiles(P, s));
+        before.push_back(before.back() + (long long)s.tiles * s.chunks * P.n_kv);
     }
-    const long long total = before.back();
+    if (before.back() > 0x3fffffffll) return 0;   // refused by the host
+    const int total = (int)before.back();
     if (total == 0) return 0;
-    const int sharers = tree_sharers(total, blocks);
-    long long next = 0;
+    const TreeCut cut(total, blocks);
+    int next = 0;
     std::map<std::tuple<int, int, int>, std::vector<std::pair<int, int>>> parts;   // item -> (block, which of its partial results)
     for (int k = 0; k < blocks; ++k) {
-        const long long t0 = tree_share(total, k, sharers), t1 = tree_share(total, k + 1, sharers);
-        if (t0 != next || t1 < t0 || (k < sharers && t1 == t0) || (k >= sharers && t1 != t0)) return 4;
-        if (k < sharers && t1 - t0 > total / sharers + 1) return 5;
+        const int t0 = cut.begin(k), t1 = cut.begin(k + 1);
+        if (t0 != next || t1 < t0 || t1 - t0 > total / blocks + 1 || t1 - t0 < total / blocks) return 4;
         if (t0 == t1) continue;
         int b = 0;
         while (before[b + 1] <= t0) ++b;
         TreeCursor c;
-        c.start(P, b, t0 - before[b], t1 - t0);
+        c.start(P, b, tree_seq(P, b), (int)(t0 - before[b]), t1 - t0);
         int item = 0;
         while (c.left > 0) {
             if (c.s.tiles == 0 || c.b >= P.n_seqs || c.h >= P.n_kv || c.c >= c.s.chunks || c.tile >= c.s.tiles) return 6;
@@ -47,7 +47,7 @@ static int check(const TreeLists& P, int blocks) {
             const long long at = before[c.b] + ((long long)c.h * c.s.chunks + c.c) * c.s.tiles + c.tile;
             if (at != next) return 7;
             for (int i = 0; i < n; ++i)
-                if (tree_owner(total, at + i, sharers) != k) return 8;
+                if (cut.owner((int)at + i) != k) return 8;
             if (n != c.s.tiles) parts[{c.b, c.h, c.c}].push_back({k, item ? 1 : 0});
             if (n != c.s.tiles && item && c.left != n) return 9;   // a partial item that is not the block's first is its last
             next += n;
@@ -60,8 +60,8 @@ static int check(const TreeLists& P, int blocks) {
     for (auto& it : parts) {
         const TreeSeq s = tree_seq(P, std::get<0>(it.first));
         const long long tile0 = before[std::get<0>(it.first)] + ((long long)std::get<1>(it.first) * s.chunks + std::get<2>(it.first)) * s.tiles;
-        const int k0 = tree_owner(total, tile0, sharers), k1 = tree_owner(total, tile0 + s.tiles - 1, sharers);
-        const bool late = tree_share(total, k0, sharers) < tile0;
+        const int k0 = cut.owner((int)tile0), k1 = cut.owner((int)tile0 + s.tiles - 1);
+        const bool late = cut.begin(k0) < tile0;
         if ((int)it.second.size() != k1 - k0 + 1) return 12;
         for (int i = 0; i < (int)it.second.size(); ++i)
             if (it.second[i].first != k0 + i || it.second[i].second != (i == 0 && late ? 1 : 0)) return 13;
