@@ -224,7 +224,7 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     const int hd = pages->head_dim, g = a->n_q_heads / pages->n_kv_heads;
     const long long rows = (long long)min(a->n_rows, SDV_TREE_ROWS) * g, chunks = (rows + kTreeTileRows - 1) / kTreeTileRows;
     const long long units = (((long long)a->n_rows * g + 3) / 4 + a->n_seqs) * pages->n_kv_heads;   // of the merge
-    if ((long long)a->n_rows * a->n_q_heads > INT_MAX / 2 || units * (hd / 32) > INT_MAX) return SDV_EINVAL;
+    if ((long long)a->n_rows * a->n_q_heads > INT_MAX / 2 || units * (hd / 16) > INT_MAX) return SDV_EINVAL;
     const long long keys = min((long long)a->table_width * pages->page_size, (long long)INT_MAX);
     const long long each = ((keys + kTreeKeys - 1) / kTreeKeys) * chunks * pages->n_kv_heads, most = each * min(a->n_seqs, a->n_rows);   // no more tiles than this
     if (each * a->n_seqs > INT_MAX / 2) return SDV_EINVAL;   // (whatever cu_rows holds)
@@ -266,10 +266,10 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     if (!make_page_map(&map_k, pages->k, pages, box_keys) || !make_page_map(&map_v, pages->v, pages, box_keys)) return SDV_EINVAL;
     const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, false, map_k, map_v, P);
     if (first != SDV_OK || P.blocks == 1) return first;   // one block does everything alone
-    // Merge: units of four (row, head) pairs, of 32 columns where that leaves no more than three blocks an SM (see tree_merge_kernel); as many at a time for a block
+    // Merge: units of four (row, head) pairs, of 16 columns where that leaves no more than three blocks an SM (see tree_merge_kernel); as many at a time for a block
     // as three blocks an SM need.
     const long long room = (long long)sm_count(dev) * 3;
-    const int split = units * (hd / 32) <= room ? hd / 32 : 1;
+    const int split = units * (hd / 16) <= room ? hd / 16 : 1;
     const int group = (int)min((long long)kMergeWarps, (units * split + room - 1) / room);
     return launch(merge_kernel(pages->dtype, hd), (int)min((units * split + group - 1) / group, room), kMergeThreads, 0, cuda_stream, 1, true, P, group, split);
 }

@@ -521,8 +521,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
 }
 
 // Output rows whose keys several blocks went through: un-normalised partial outputs weighted by 2^(maximum - largest maximum).  A unit is four tile rows of an
-// item, 32 columns of them when `split`, which is where there are few units; a lane has four columns of one row.  A warp takes a unit; those with more than ten
-// parts are gone through by whole blocks (a long cache of few sequences is cut into up to 150 parts).  Neighbouring units are in different blocks, so that a long
+// item, or 16 columns of them where there are so few units that each has a block; a lane has four columns of one row.  A warp takes a unit; those with more than
+// twelve parts, and the fine ones, are gone through by whole blocks (a long cache of few sequences is cut into up to 150 parts).  Neighbouring units are in different blocks, so that a long
 // sequence among short ones has many blocks' help.  Where the parts are follows from the lengths alone and is worked out before the attention is waited for.
 // Bound by latency: launch, a round trip to L2 for five parts, the store.
 constexpr int kMergeWarps = 8, kMergeThreads = kMergeWarps * 32, kMergeDeep = 5 /* parts a warp has in flight */, kMergeFew = 12;
@@ -593,6 +593,8 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
     __shared__ float4 shared_o[kMergeWarps][32];
     __shared__ float2 shared_ml[kMergeWarps][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, my_row = (lane >> 1) & 3;
+    const bool fine = split * 16 == HD;
+    const int place = fine ? lane & 15 : lane, few = fine ? 1 : kMergeFew;
     // Rows of units are numbered by the (row, query head) pairs of a KV head in fours, those of a sequence beginning a new one.  (The host sees to it that
     // the number of units stays within 32 bits.)
     const auto first_unit = [&](int b) { return (int)((unsigned)(rows_begin(P.cu_rows, b, P.n_rows) * P.g + 3) / 4u) + b; };
@@ -645,12 +647,11 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
         bool many = false;
         if (warp < group) {
             const TreeUnit& q = shared_unit[warp];
-            many = q.n > kMergeFew;
+            many = q.n > few;
             if (q.n > 1 && !many) {
                 TreeMergeRow<T, HD> row(P, q, my_row, lane);
 #pragma unroll 1
-                for (int c = q.col; c < q.col + cols; c += 64) {   // two groups of 32 columns (split: one)
-                    const bool wide = cols > 32;
+                for (int c = 0; c < HD; c += 64) {   // two groups of 32 columns
                     float m = -CUDART_INF_F, l = 0.f;
                     float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll 1
@@ -660,57 +661,57 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
                         const float2 a = __ldcg(row.ml + at), b = two ? __ldcg(row.ml + next) : make_float2(-CUDART_INF_F, 0.f);
                         float4 x[2], y[2];
 #pragma unroll
-                        for (int g = 0; g < 2; ++g)
-                            if (g == 0 || wide) {
-                                x[g] = __ldcg(reinterpret_cast<const float4*>(row.o + at * HD + (c + g * 32) * 4));
-                                if (two) y[g] = __ldcg(reinterpret_cast<const float4*>(row.o + next * HD + (c + g * 32) * 4));
-                            }
+                        for (int g = 0; g < 2; ++g) {
+                            x[g] = __ldcg(reinterpret_cast<const float4*>(row.o + at * HD + (c + g * 32) * 4));
+                            if (two) y[g] = __ldcg(reinterpret_cast<const float4*>(row.o + next * HD + (c + g * 32) * 4));
+                        }
                         const float mx = fmaxf(m, fmaxf(a.x, b.x)), ref = mx == -CUDART_INF_F ? 0.f : mx, keep = exp2f(m - ref), fa = exp2f(a.x - ref), fb = exp2f(b.x - ref);
                         m = mx;
                         l = l * keep + fa * a.y + fb * b.y;
 #pragma unroll
-                        for (int g = 0; g < 2; ++g)
-                            if (g == 0 || wide) {
-                                tree_scale(o[g], keep);
-                                tree_add(o[g], fa, x[g]);
-                                if (two) tree_add(o[g], fb, y[g]);
-                            }
+                        for (int g = 0; g < 2; ++g) {
+                            tree_scale(o[g], keep);
+                            tree_add(o[g], fa, x[g]);
+                            if (two) tree_add(o[g], fb, y[g]);
+                        }
                     }
 #pragma unroll
-                    for (int g = 0; g < 2; ++g)
-                        if (g == 0 || wide) row.store(P, q, my_row, lane, c + g * 32, o[g], l);
+                    for (int g = 0; g < 2; ++g) row.store(P, q, my_row, lane, c + g * 32, o[g], l);
                 }
             }
         }
         if (!__syncthreads_or(many)) continue;
-        // those with many parts, one after the other: as many columns at once as a unit has (in groups of 32), the parts shared out among the warps that remain for each
-        const int groups = cols / 32, step = kMergeWarps / groups;
+        // Together, one unit after the other.  Fine units: every half warp has parts of its own.  Others: warps in turn have a group of 32 columns, and the parts are shared out among
+        // those of a group.
+        const int groups = fine ? 1 : cols / 32, halves = fine ? 2 : 1, step = kMergeWarps / groups * halves;
 #pragma unroll 1
         for (int k = 0; k < group; ++k) {
             const TreeUnit& q = shared_unit[k];
-            if (q.n <= kMergeFew) continue;   // the same for the whole block
-            TreeMergeRow<T, HD> row(P, q, my_row, lane);
+            if (q.n <= few) continue;   // the same for the whole block
+            TreeMergeRow<T, HD> row(P, q, my_row, place);
             const int c = q.col + warp % groups * 32;
             float m = -CUDART_INF_F, l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-            for (int i0 = warp / groups; i0 < q.n; i0 += kMergeDeep * step) tree_gather<HD>(P, q, row.ml, row.o + c * 4, i0, step, m, l, o);
+            for (int i0 = warp / groups * halves + (fine ? lane >> 4 : 0); i0 < q.n; i0 += kMergeDeep * step) tree_gather<HD>(P, q, row.ml, row.o + c * 4, i0, step, m, l, o);
             shared_o[warp][lane] = o;
             shared_ml[warp][lane] = make_float2(m, l);
             __syncthreads();
             if (warp < groups) {
+                // fine: half a warp's lanes add up the other half's as well
                 float mx = -CUDART_INF_F, sum = 0.f;
-                for (int t = warp; t < kMergeWarps; t += groups) mx = fmaxf(mx, shared_ml[t][lane].x);
+                for (int t = warp; t < kMergeWarps; t += groups) mx = fmaxf(mx, fmaxf(shared_ml[t][lane].x, shared_ml[t][lane ^ (halves - 1) * 16].x));
                 const float ref = mx == -CUDART_INF_F ? 0.f : mx;
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-                for (int t = warp; t < kMergeWarps; t += groups) {
-                    const float2 ml = shared_ml[t][lane];
+                for (int t = 0; t < kMergeWarps / groups * halves; ++t) {
+                    const int w = warp + (t / halves) * groups, at = lane ^ (t & (halves - 1)) * 16;
+                    const float2 ml = shared_ml[w][at];
                     const float f = exp2f(ml.x - ref);
                     sum += f * ml.y;
-                    tree_add(v, f, shared_o[t][lane]);
+                    tree_add(v, f, shared_o[w][at]);
                 }
-                row.store(P, q, my_row, lane, c, v, sum);
+                if (place == lane) row.store(P, q, my_row, place, c, v, sum);
             }
             __syncthreads();
         }
