@@ -77,14 +77,13 @@ bool pages_ok(const sdv_pages* p, int dev) {
 }
 
 typedef void (*RopeKernel)(const sdv_rope_args, const sdv_pages, int);
-template <typename T, bool I>
-RopeKernel rope_kernel(int w) {
-    return w == 8 ? rope_append_kernel<T, I, 8> : w == 4 ? rope_append_kernel<T, I, 4> : w == 2 ? rope_append_kernel<T, I, 2> : rope_append_kernel<T, I, 1>;
+template <typename T>
+RopeKernel rope_kernel(bool interleaved, bool wide) {
+    return interleaved ? wide ? rope_append_kernel<T, true, 8> : rope_append_kernel<T, true, 1> : wide ? rope_append_kernel<T, false, 8> : rope_append_kernel<T, false, 1>;
 }
-RopeKernel rope_kernel(int dtype, bool interleaved, int w) {
-    if (dtype == SDV_BF16) return interleaved ? rope_kernel<__nv_bfloat16, true>(w) : rope_kernel<__nv_bfloat16, false>(w);
-    return interleaved ? rope_kernel<__half, true>(w) : rope_kernel<__half, false>(w);
-}
+RopeKernel rope_kernel(int dtype, bool interleaved, bool wide) { return dtype == SDV_BF16 ? rope_kernel<__nv_bfloat16>(interleaved, wide) : rope_kernel<__half>(interleaved, wide); }
+typedef void (*RopeStaged)(const sdv_rope_args, const sdv_pages, int, int);
+RopeStaged rope_staged(int dtype) { return dtype == SDV_BF16 ? rope_staged_kernel<__nv_bfloat16> : rope_staged_kernel<__half>; }
 
 typedef void (*TreeKernel)(const CUtensorMap, const CUtensorMap, const TreeParams);
 typedef void (*MergeKernel)(const TreeParams, int, int);
@@ -108,8 +107,8 @@ int prepare_device(int dev) {
         load((const void*)paged_slots_kernel);
         load((const void*)verify_sampled_kernel);
         for (int t = SDV_BF16; t <= SDV_FP16; ++t) {
-            for (int w = 1; w <= 8; w *= 2)
-                for (int i = 0; i < 2; ++i) load((const void*)rope_kernel(t, i != 0, w));
+            for (int i = 0; i < 4; ++i) load((const void*)rope_kernel(t, (i & 1) != 0, (i & 2) != 0));
+            load((const void*)rope_staged(t));
             for (int hd = 64; hd <= 128; hd += 64) {
                 load((const void*)merge_kernel(t, hd));
                 if (r == cudaSuccess) r = cudaFuncSetAttribute((const void*)tree_kernel(t, hd), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tree_smem(hd));
@@ -187,15 +186,20 @@ int sdv_rope_append(const sdv_rope_args* a, const sdv_pages* pages, void* cuda_s
     }
     const int rc = prepare_device(dev);
     if (rc != SDV_OK) return rc;
-    // elements moved at once: as many as the pairs' two halves, the strides and the addresses allow
+    // Eight elements at once where rows begin on 16-byte boundaries, one otherwise.  The two halves of a rotated head that are no multiple of eight go through shared memory.
     const int half = a->rot_dim / 2;
-    int w = 8;
-    while (w > 1 && (half % w || a->head_dim % (2 * w) || (bits & (uintptr_t)(w - 1)))) w /= 2;
-    // rows of a block: about four units a thread, fewer while there are blocks to spare (8191 rows of 24 + 8 heads: 29.7 us with two to four rows a block, 33.6 with six)
-    const int units = ((a->q ? a->n_q_heads : 0) + (a->k ? 2 * a->n_kv_heads : 0)) * (a->head_dim / (2 * w));
+    const bool aligned = (bits & 7) == 0 && a->head_dim % 8 == 0, wide = aligned && a->head_dim % 16 == 0 && (a->interleaved || half % 8 == 0);
+    // rows of a block: about four units of 16 elements a thread, fewer while there are blocks to spare (8191 rows of 24 + 8 heads: 29.7 us with two to four rows a block, 33.6
+    // with six)
+    const int heads = (a->q ? a->n_q_heads : 0) + (a->k ? 2 * a->n_kv_heads : 0), units = max(1, heads * a->head_dim / 16);
     const int tokens = max(1, min(min(8, 4 * kRopeThreads / units), a->n_rows / (sm_count(dev) * 8)));
-    return launch(rope_kernel(a->dtype, a->interleaved != 0, w), (a->n_rows + tokens - 1) / tokens, kRopeThreads, (size_t)tokens * half * sizeof(float2), cuda_stream, 1, false, *a,
-                  a->k ? *pages : none, tokens);
+    const int grid = (a->n_rows + tokens - 1) / tokens;
+    if (aligned && !wide && !a->interleaved) {
+        const int staged = min(heads - (a->k ? a->n_kv_heads : 0), 16384 / a->head_dim);   // 32 KB of heads at most
+        return launch(rope_staged(a->dtype), grid, kRopeThreads, (size_t)staged * a->head_dim * 2 + (size_t)tokens * half * sizeof(float2), cuda_stream, 1, false, *a, a->k ? *pages : none,
+                      tokens, staged);
+    }
+    return launch(rope_kernel(a->dtype, a->interleaved != 0, wide), grid, kRopeThreads, (size_t)tokens * half * sizeof(float2), cuda_stream, 1, false, *a, a->k ? *pages : none, tokens);
 }
 
 size_t sdv_tree_attention_workspace_bytes(int n_seqs, int head_dim) {

@@ -161,7 +161,6 @@ template <> struct Half16<__half> {
 // W 16-bit elements moved at once.
 template <int W> struct Words;
 template <> struct Words<8> { typedef uint4 type; };
-template <> struct Words<4> { typedef uint2 type; };
 template <> struct Words<2> { typedef uint32_t type; };
 template <> struct Words<1> { typedef uint16_t type; };
 template <typename T, int W>
@@ -171,13 +170,9 @@ union Elements {
     __device__ __forceinline__ Elements() {}
 };
 
-// A block takes `tokens` rows: their cosines and sines once (an angle is worked out in 64 bits as a fraction of a turn: a position of 10^6 in fp32 is off by up
-// to 0.03 rad), then all heads of q, k and v in units of 2 W elements, W on either side of the pairs.  A unit is read whole before it is written, so q may be turned in place.
-// Bound by memory for prompts, by latency for the rows of a step.
-template <typename T, bool INTERLEAVED, int W>
-__global__ void __launch_bounds__(kRopeThreads, 8) rope_append_kernel(const __grid_constant__ sdv_rope_args a, const __grid_constant__ sdv_pages pages, int tokens) {
-    extern __shared__ float2 turn[];   // [token][pair] cosine, sine
-    const int half = a.rot_dim / 2, t0 = (int)blockIdx.x * tokens, n = min(tokens, a.n_rows - t0);
+// Cosines and sines of n rows from row t0 on, [row][pair].  An angle is worked out in 64 bits as a fraction of a turn: a position of 10^6 in fp32 is off by up to 0.03 rad.
+__device__ __forceinline__ void rope_turns(const sdv_rope_args& a, int t0, int n, float2* turn) {
+    const int half = a.rot_dim / 2;
     for (int i = threadIdx.x; i < n * half; i += kRopeThreads) {
         const int t = i / half, p = i - t * half;
         const double turns = (double)__ldg(a.positions + t0 + t) * __ldg(a.frequencies + p) * 0.15915494309189533577;   // 1 / (2 pi)
@@ -185,9 +180,34 @@ __global__ void __launch_bounds__(kRopeThreads, 8) rope_append_kernel(const __gr
         sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
         turn[i] = make_float2(c * a.factor, s * a.factor);
     }
+}
+
+template <typename T>
+__device__ __forceinline__ void rope_turn(T& lo, T& hi, float2 cs) {
+    const float b = Half16<T>::up(lo), d = Half16<T>::up(hi);
+    lo = Half16<T>::down(b * cs.x - d * cs.y);
+    hi = Half16<T>::down(d * cs.x + b * cs.y);
+}
+
+// Where row r of a head goes in the pages; null: nowhere.
+template <typename T>
+__device__ __forceinline__ T* rope_place(const sdv_rope_args& a, const sdv_pages& pages, void* base, int r, int h) {
+    const int slot = __ldg(a.slots + r);
+    if (slot < 0 || slot >= (long long)pages.n_pages * pages.page_size) return nullptr;
+    const int page = slot / pages.page_size, token = slot - page * pages.page_size;
+    return (T*)base + page * pages.page_stride + h * pages.head_stride + token * pages.token_stride;
+}
+
+// A block takes `tokens` rows: their cosines and sines once, then all heads of q, k and v in units of 2 W elements, W on either side of the pairs (half layout: only where
+// the halves are multiples of W) or W neighbouring pairs.  A unit is read whole before it is written, so q may be turned in place.
+// Bound by memory for prompts (8191 rows of 24 + 8 heads of 128: 29.7 us, 5.66 TB/s), by latency for the rows of a step.
+template <typename T, bool INTERLEAVED, int W>
+__global__ void __launch_bounds__(kRopeThreads, 8) rope_append_kernel(const __grid_constant__ sdv_rope_args a, const __grid_constant__ sdv_pages pages, int tokens) {
+    extern __shared__ float2 turn[];   // [token][pair] cosine, sine
+    const int half = a.rot_dim / 2, t0 = (int)blockIdx.x * tokens, n = min(tokens, a.n_rows - t0);
+    rope_turns(a, t0, n, turn);
     __syncthreads();
     const int per_head = a.head_dim / (2 * W), q_units = a.q ? a.n_q_heads * per_head : 0, k_units = a.k ? a.n_kv_heads * per_head : 0, units = q_units + 2 * k_units;
-    const long long capacity = (long long)pages.n_pages * pages.page_size;
     for (int i = threadIdx.x; i < n * units; i += kRopeThreads) {
         const int t = i / units, r = t0 + t;
         int u = i - t * units;
@@ -200,11 +220,9 @@ __global__ void __launch_bounds__(kRopeThreads, 8) rope_append_kernel(const __gr
             src = (const T*)a.q + r * a.q_row_stride + h * a.q_head_stride;
             dst = (T*)a.q_out + r * a.out_row_stride + h * a.out_head_stride;
         } else {
-            const int slot = __ldg(a.slots + r);
-            if (slot < 0 || slot >= capacity) continue;
-            const int page = slot / pages.page_size, token = slot - page * pages.page_size;
             src = is_v ? (const T*)a.v + r * a.v_row_stride + h * a.v_head_stride : (const T*)a.k + r * a.k_row_stride + h * a.k_head_stride;
-            dst = (T*)(is_v ? pages.v : pages.k) + page * pages.page_stride + h * pages.head_stride + token * pages.token_stride;
+            dst = rope_place<T>(a, pages, is_v ? pages.v : pages.k, r, h);
+            if (!dst) continue;
         }
         // elements e0 .. and e1 .. of the head; pairs p .. p + W - 1 where they are turned
         const int pair = at * W;
@@ -222,16 +240,83 @@ __global__ void __launch_bounds__(kRopeThreads, 8) rope_append_kernel(const __gr
             const float2* cs = turn + t * half + pair;
 #pragma unroll
             for (int j = 0; j < W; ++j) {
+                if (INTERLEAVED && W > 1 && pair + j >= half) break;
                 // the pair's members: in the half layout x[j], y[j]; interleaved, neighbours in the 2 W elements x, y
                 T& lo = INTERLEAVED ? (2 * j < W ? x.e[(2 * j) % W] : y.e[(2 * j) % W]) : x.e[j];
                 T& hi = INTERLEAVED ? (2 * j + 1 < W ? x.e[(2 * j + 1) % W] : y.e[(2 * j + 1) % W]) : y.e[j];
-                const float b = Half16<T>::up(lo), d = Half16<T>::up(hi);
-                lo = Half16<T>::down(b * cs[j].x - d * cs[j].y);
-                hi = Half16<T>::down(d * cs[j].x + b * cs[j].y);
+                rope_turn(lo, hi, cs[j]);
             }
         }
         *reinterpret_cast<Word*>(dst + e0) = x.w;
         *reinterpret_cast<Word*>(dst + e1) = y.w;
+    }
+}
+
+// Half layout with halves that are no multiple of eight: the partners of eight aligned elements do not lie on a 16-byte boundary.  The heads of q and k go through shared memory,
+// `heads` of a row at a time, and are turned there in place, two pairs a thread; global memory sees 16-byte accesses only.  A thread keeps its place within the heads and
+// steps from head to head without a division.  (Two bytes at a time from global memory, 51 pairs took 123 us where 56 took 32.)
+template <typename T>
+__global__ void __launch_bounds__(kRopeThreads, 8) rope_staged_kernel(const __grid_constant__ sdv_rope_args a, const __grid_constant__ sdv_pages pages, int tokens, int heads) {
+    extern __shared__ uint4 stage[];   // [head][16 bytes] | [token][pair] cosine, sine
+    const int half = a.rot_dim / 2, t0 = (int)blockIdx.x * tokens, n = min(tokens, a.n_rows - t0), per_head = a.head_dim / 8, words = (half + 1) / 2;
+    float2* turn = reinterpret_cast<float2*>(stage + heads * per_head);
+    rope_turns(a, t0, n, turn);
+    const int q_heads = a.q ? a.n_q_heads : 0, k_heads = a.k ? a.n_kv_heads : 0;
+    const int my_head = (int)threadIdx.x / per_head, my_chunk = (int)threadIdx.x - my_head * per_head, head_step = kRopeThreads / per_head;   // 16 bytes of a head (at most 32)
+    const int my_row = (int)threadIdx.x / words, my_pair = ((int)threadIdx.x - my_row * words) * 2, row_step = kRopeThreads / words;           // two pairs (at most 64)
+    for (int t = 0; t < n; ++t) {
+        const int r = t0 + t;
+        const float2* cs = turn + t * half + my_pair;
+        for (int h0 = 0; h0 < q_heads + k_heads; h0 += heads) {
+            const int count = min(heads, q_heads + k_heads - h0);
+            if (my_head < head_step) {
+                for (int h = my_head; h < count; h += head_step) {
+                    const int hd = h0 + h;
+                    const T* src = hd < q_heads ? (const T*)a.q + r * a.q_row_stride + hd * a.q_head_stride : (const T*)a.k + r * a.k_row_stride + (hd - q_heads) * a.k_head_stride;
+                    stage[h * per_head + my_chunk] = *reinterpret_cast<const uint4*>(src + my_chunk * 8);
+                }
+            }
+            __syncthreads();
+            if (my_row < row_step) {
+                const bool two = my_pair + 1 < half;
+                const float2 c0 = cs[0], c1 = two ? cs[1] : c0;
+                for (int h = my_row; h < count; h += row_step) {
+                    T* lo = reinterpret_cast<T*>(stage + h * per_head) + my_pair;
+                    T* hi = lo + half;
+                    if (two) {
+                        Elements<T, 2> x, y;
+                        x.w = *reinterpret_cast<const uint32_t*>(lo);
+                        y.e[0] = hi[0];
+                        y.e[1] = hi[1];
+                        rope_turn(x.e[0], y.e[0], c0);
+                        rope_turn(x.e[1], y.e[1], c1);
+                        *reinterpret_cast<uint32_t*>(lo) = x.w;
+                        hi[0] = y.e[0];
+                        hi[1] = y.e[1];
+                    } else {   // the last of an odd number of pairs
+                        T x = lo[0], y = hi[0];
+                        rope_turn(x, y, c0);
+                        lo[0] = x;
+                        hi[0] = y;
+                    }
+                }
+            }
+            __syncthreads();
+            if (my_head < head_step) {
+                for (int h = my_head; h < count; h += head_step) {
+                    const int hd = h0 + h;
+                    T* dst = hd < q_heads ? (T*)a.q_out + r * a.out_row_stride + hd * a.out_head_stride : rope_place<T>(a, pages, pages.k, r, hd - q_heads);
+                    if (dst) *reinterpret_cast<uint4*>(dst + my_chunk * 8) = stage[h * per_head + my_chunk];
+                }
+            }
+            __syncthreads();
+        }
+        if (my_head < head_step) {
+            for (int h = my_head; h < k_heads; h += head_step) {   // values are only moved
+                T* dst = rope_place<T>(a, pages, pages.v, r, h);
+                if (dst) *reinterpret_cast<uint4*>(dst + my_chunk * 8) = *reinterpret_cast<const uint4*>((const T*)a.v + r * a.v_row_stride + h * a.v_head_stride + my_chunk * 8);
+            }
+        }
     }
 }
 

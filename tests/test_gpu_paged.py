@@ -154,6 +154,10 @@ def check_rope(got, x, pos, f, factor, interleaved, what):
     ("bfloat16", 1300, 5, 1, 256, 256, 128, False, 2),
     ("bfloat16", 3000, 4, 2, 64, 64, 32, True, 0),
     ("float16", 20, 1, 1, 2, 2, 8, False, 0),
+    ("bfloat16", 3, 66, 4, 256, 102, 16, False, 0),    # more heads than shared memory takes at a time
+    ("float16", 2500, 7, 1, 96, 90, 16, True, 0),
+    ("bfloat16", 40, 3, 3, 72, 64, 8, False, 0),       # heads that are no multiple of sixteen
+    ("float16", 30, 2, 1, 88, 86, 16, False, 8),
 ])
 def test_rope_append(dtype, n, hq, hkv, hd, rot, page, tokens_first, offset, interleaved):
     import torch
