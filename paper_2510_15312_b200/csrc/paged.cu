@@ -43,9 +43,9 @@ int sm_count(int dev) {
     return n;
 }
 
-// A launch, in clusters of `cluster` blocks, `dependent`: one that may overlap the tail of the kernel before it.
+// A launch, in clusters of `cluster` blocks, that may overlap the tail of the kernel before it: each kernel waits for that one's end before it reads what it may have written.
 template <typename... KArgs, typename... Args>
-int launch(void (*kernel)(KArgs...), int grid, int block, size_t smem, void* stream, int cluster, bool dependent, const Args&... args) {
+int launch(void (*kernel)(KArgs...), int grid, int block, size_t smem, void* stream, int cluster, const Args&... args) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3((unsigned)grid);
@@ -53,19 +53,14 @@ int launch(void (*kernel)(KArgs...), int grid, int block, size_t smem, void* str
     cfg.dynamicSmemBytes = smem;
     cfg.stream = (cudaStream_t)stream;
     cudaLaunchAttribute at[2];
-    int n = 0;
-    if (cluster > 1) {
-        at[n].id = cudaLaunchAttributeClusterDimension;
-        at[n].val.clusterDim.x = (unsigned)cluster;
-        at[n].val.clusterDim.y = 1;
-        at[n++].val.clusterDim.z = 1;
-    }
-    if (dependent) {
-        at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at[n++].val.programmaticStreamSerializationAllowed = 1;
-    }
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = (unsigned)n;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? SDV_OK : SDV_ECUDA;
 }
 
@@ -160,7 +155,7 @@ int sdv_paged_slots(const sdv_slots_args* a, void* cuda_stream) {
     if (rc != SDV_OK) return rc;
     const long long items = (long long)a->n_rows + min((long long)a->n_free, (long long)a->n_seqs * a->table_width);
     const int grid = (int)max(1ll, min((items + kSlotThreads - 1) / kSlotThreads, (long long)sm_count(dev)));
-    return launch(paged_slots_kernel, grid, kSlotThreads, 0, cuda_stream, 1, false, *a);
+    return launch(paged_slots_kernel, grid, kSlotThreads, 0, cuda_stream, 1, *a);
 }
 
 int sdv_rope_append(const sdv_rope_args* a, const sdv_pages* pages, void* cuda_stream) {
@@ -196,10 +191,10 @@ int sdv_rope_append(const sdv_rope_args* a, const sdv_pages* pages, void* cuda_s
     const int grid = (a->n_rows + tokens - 1) / tokens;
     if (aligned && !wide && !a->interleaved) {
         const int staged = min(heads - (a->k ? a->n_kv_heads : 0), 16384 / a->head_dim);   // 32 KB of heads at most
-        return launch(rope_staged(a->dtype), grid, kRopeThreads, (size_t)staged * a->head_dim * 2 + (size_t)tokens * half * sizeof(float2), cuda_stream, 1, false, *a, a->k ? *pages : none,
+        return launch(rope_staged(a->dtype), grid, kRopeThreads, (size_t)staged * a->head_dim * 2 + (size_t)tokens * half * sizeof(float2), cuda_stream, 1, *a, a->k ? *pages : none,
                       tokens, staged);
     }
-    return launch(rope_kernel(a->dtype, a->interleaved != 0, wide), grid, kRopeThreads, (size_t)tokens * half * sizeof(float2), cuda_stream, 1, false, *a, a->k ? *pages : none, tokens);
+    return launch(rope_kernel(a->dtype, a->interleaved != 0, wide), grid, kRopeThreads, (size_t)tokens * half * sizeof(float2), cuda_stream, 1, *a, a->k ? *pages : none, tokens);
 }
 
 size_t sdv_tree_attention_workspace_bytes(int n_seqs, int head_dim) {
@@ -268,14 +263,14 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     CUtensorMap map_k, map_v;
     const int box_keys = min(pages->page_size, kTreeKeys);
     if (!make_page_map(&map_k, pages->k, pages, box_keys) || !make_page_map(&map_v, pages->v, pages, box_keys)) return SDV_EINVAL;
-    const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, false, map_k, map_v, P);
+    const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, map_k, map_v, P);
     if (first != SDV_OK || P.blocks == 1) return first;   // one block does everything alone
     // Merge: units of four (row, head) pairs, of 16 columns where that leaves no more than three blocks an SM (see tree_merge_kernel); as many at a time for a block
     // as three blocks an SM need.
     const long long room = (long long)sm_count(dev) * 3;
     const int split = units * (hd / 16) <= room ? hd / 16 : 1;
     const int group = (int)min((long long)kMergeWarps, (units * split + room - 1) / room);
-    return launch(merge_kernel(pages->dtype, hd), (int)min((units * split + group - 1) / group, room), kMergeThreads, 0, cuda_stream, 1, true, P, group, split);
+    return launch(merge_kernel(pages->dtype, hd), (int)min((units * split + group - 1) / group, room), kMergeThreads, 0, cuda_stream, 1, P, group, split);
 }
 
 int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {
@@ -294,7 +289,7 @@ int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {
     int cs = 1;
     while (cs < kVerifyMaxCluster && tiles >= 2 * cs * kVerifyWarps && (long long)a->n_seqs * cs * 2 <= 2ll * sm_count(dev)) cs *= 2;
     const int per = (tiles + cs - 1) / cs;
-    return launch(verify_sampled_kernel, a->n_seqs * cs, kVerifyThreads, (size_t)per * sizeof(double), cuda_stream, cs, false, *a, per);
+    return launch(verify_sampled_kernel, a->n_seqs * cs, kVerifyThreads, (size_t)per * sizeof(double), cuda_stream, cs, *a, per);
 }
 
 }  // extern "C"

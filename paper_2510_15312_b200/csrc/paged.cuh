@@ -45,6 +45,8 @@ __device__ __forceinline__ long long slots_want(const sdv_slots_args& a, int b, 
 __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_constant__ sdv_slots_args a) {
     __shared__ SlotShared s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = a.n_seqs;
+    grid_dep_wait();
+    grid_dep_launch();   // behind the wait: what comes next may rely on all that came before
     const int head = max(__ldg(a.free_state), 0);
     // needs of this thread's sequences, summed up over the block.  The sum of all needs stays below 2^31: each is at most
     // table_width, and the host refuses n_seqs * table_width beyond that.
@@ -173,6 +175,8 @@ union Elements {
 // Cosines and sines of n rows from row t0 on, [row][pair].  An angle is worked out in 64 bits as a fraction of a turn: a position of 10^6 in fp32 is off by up to 0.03 rad.
 __device__ __forceinline__ void rope_turns(const sdv_rope_args& a, int t0, int n, float2* turn) {
     const int half = a.rot_dim / 2;
+    grid_dep_wait();
+    grid_dep_launch();   // behind the wait: what comes next may rely on all that came before
     for (int i = threadIdx.x; i < n * half; i += kRopeThreads) {
         const int t = i / half, p = i - t * half;
         const double turns = (double)__ldg(a.positions + t0 + t) * __ldg(a.frequencies + p) * 0.15915494309189533577;   // 1 / (2 pi)

@@ -193,12 +193,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     }
     if (warp == 5) tmem_alloc(&ctl->tmem_base, 256);   // S0 | S1, 64 columns each | O, HD columns
     if (warp == 4 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &map_v : &map_k) : "memory");
+    grid_dep_wait();
     ctl->scan.fill(P);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctl->tmem_base;
-    grid_dep_launch();
+    grid_dep_launch();   // behind the wait: the merge reads the lengths at once
     TreeCursor cur;
     {
         const TreeCut cut(ctl->scan.total(), P.blocks);
@@ -641,7 +642,10 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
             }
             if (lane == 0) shared_unit[warp] = q;
         }
-        if (!waited) grid_dep_wait();   // the parts are there
+        if (!waited) {
+            grid_dep_wait();   // the parts are there
+            grid_dep_launch();
+        }
         waited = true;
         __syncwarp();
         bool many = false;

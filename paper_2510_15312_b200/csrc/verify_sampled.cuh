@@ -72,6 +72,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_sampled_kernel(const
     __shared__ double sums[2][kVerifyMaxCluster];   // of every block's share
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int CS = (int)cluster_size(), rank = (int)cluster_rank(), b = (int)blockIdx.x / CS;
+    grid_dep_wait();
+    grid_dep_launch();   // behind the wait: what comes next may rely on all that came before
     const int first = rows_begin(a.cu_rows, b, a.n_rows), all = rows_count(a.cu_rows, b, a.n_rows), T = min(all, SDV_TREE_ROWS);
     if (blockIdx.x == 0) {   // rows of no sequence
         const int from = rows_begin(a.cu_rows, a.n_seqs, a.n_rows), until = rows_begin(a.cu_rows, 0, a.n_rows);
