@@ -80,7 +80,7 @@ RopeKernel rope_kernel(int dtype, bool interleaved, bool wide) { return dtype ==
 typedef void (*RopeStaged)(const sdv_rope_args, const sdv_pages, int, int);
 RopeStaged rope_staged(int dtype) { return dtype == SDV_BF16 ? rope_staged_kernel<__nv_bfloat16> : rope_staged_kernel<__half>; }
 
-typedef void (*TreeKernel)(const CUtensorMap, const CUtensorMap, const TreeParams);
+typedef void (*TreeKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const TreeParams);
 typedef void (*MergeKernel)(const TreeParams, int, int);
 TreeKernel tree_kernel(int dtype, int hd) {
     if (dtype == SDV_BF16) return hd == 128 ? tree_attention_kernel<__nv_bfloat16, 128> : tree_attention_kernel<__nv_bfloat16, 64>;
@@ -114,16 +114,26 @@ int prepare_device(int dev) {
     return e == cudaSuccess ? SDV_OK : SDV_ECUDA;
 }
 
-// Keys (or values) as a tensor of head_dim x tokens of a page x KV heads x pages; boxes of 64 x box_keys elements, 128-byte swizzle, zeros outside.
-bool make_page_map(CUtensorMap* m, const void* base, const sdv_pages* p, int box_keys) {
+// Tensor map of 16-bit elements (strides in elements, of every dimension but the first), 128-byte swizzle, zeros outside.
+bool make_map(CUtensorMap* m, const void* base, int dtype, int rank, const long long* dims, const long long* strides, const int* box) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
-    const auto stride = [](int n, long long s) { return (cuuint64_t)(n > 1 && s ? s * 2 : 16); };   // of a dimension of one: anything valid
-    const cuuint64_t dims[4] = {(cuuint64_t)p->head_dim, (cuuint64_t)p->page_size, (cuuint64_t)p->n_kv_heads, (cuuint64_t)p->n_pages};
-    const cuuint64_t strides[3] = {stride(p->page_size, p->token_stride), stride(p->n_kv_heads, p->head_stride), stride(p->n_pages, p->page_stride)};
-    const cuuint32_t box[4] = {64, (cuuint32_t)box_keys, 1, 1}, estr[4] = {1, 1, 1, 1};
-    return fn(m, p->dtype == SDV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+    cuuint64_t d[4], s[3];
+    cuuint32_t b[4], one[4];
+    for (int i = 0; i < rank; ++i) {
+        d[i] = (cuuint64_t)dims[i];
+        b[i] = (cuuint32_t)box[i];
+        one[i] = 1;
+        if (i) s[i - 1] = (cuuint64_t)(dims[i] > 1 && strides[i - 1] ? strides[i - 1] * 2 : 16);   // of a dimension of one: anything valid
+    }
+    return fn(m, dtype == SDV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, s, b, one,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Keys (or values): head_dim x tokens of a page x KV heads x pages; boxes of 64 elements of box_keys tokens.
+bool make_page_map(CUtensorMap* m, const void* base, const sdv_pages* p, int box_keys) {
+    const long long dims[4] = {p->head_dim, p->page_size, p->n_kv_heads, p->n_pages}, strides[3] = {p->token_stride, p->head_stride, p->page_stride};
+    const int box[4] = {64, box_keys, 1, 1};
+    return make_map(m, base, p->dtype, 4, dims, strides, box);
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -207,7 +217,7 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     if (!a || !pages || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->table_width < 0) return SDV_EINVAL;
     if (pages->head_dim != 64 && pages->head_dim != 128) return SDV_EINVAL;
     if (pages->page_size < 8 || (pages->page_size & (pages->page_size - 1)) || pages->n_kv_heads < 1) return SDV_EINVAL;
-    if (a->n_q_heads < 1 || a->n_q_heads % pages->n_kv_heads || !(a->scale > 0.f) || !isfinite(a->scale)) return SDV_EINVAL;
+    if (a->n_q_heads < 1 || a->n_q_heads % pages->n_kv_heads || a->n_q_heads / pages->n_kv_heads > kTreeTileRows || !(a->scale > 0.f) || !isfinite(a->scale)) return SDV_EINVAL;
     if (a->table_stride < a->table_width && a->n_seqs > 1) return SDV_EINVAL;
     if ((a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride) & 7) return SDV_EINVAL;
     if (a->n_seqs == 0 || a->n_rows == 0 || a->table_width == 0) return SDV_OK;
@@ -221,20 +231,19 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     TreeParams P;
     memset(&P, 0, sizeof(P));
     const int hd = pages->head_dim, g = a->n_q_heads / pages->n_kv_heads;
-    const long long rows = (long long)min(a->n_rows, SDV_TREE_ROWS) * g, chunks = (rows + kTreeTileRows - 1) / kTreeTileRows;
-    const long long units = (((long long)a->n_rows * g + 3) / 4 + a->n_seqs) * pages->n_kv_heads;   // of the merge
+    const int chunk = kTreeTileRows / g, rows = min(a->n_rows, SDV_TREE_ROWS), chunks = (rows + chunk - 1) / chunk;
+    const long long units = (((long long)a->n_rows * g + 3) / 4 + a->n_rows / chunk + a->n_seqs) * pages->n_kv_heads;   // of the merge
     if ((long long)a->n_rows * a->n_q_heads > INT_MAX / 2 || units * (hd / 16) > INT_MAX) return SDV_EINVAL;
     const long long keys = min((long long)a->table_width * pages->page_size, (long long)INT_MAX);
     const long long each = ((keys + kTreeKeys - 1) / kTreeKeys) * chunks * pages->n_kv_heads, most = each * min(a->n_seqs, a->n_rows);   // no more tiles than this
     if (each * a->n_seqs > INT_MAX / 2) return SDV_EINVAL;   // (whatever cu_rows holds)
     P.blocks = (int)min((long long)tree_blocks(dev), most);
-    P.part_rows = (int)min((rows + 3) / 4 * 4, (long long)kTreeTileRows);   // in fours
+    P.part_rows = (min(rows, chunk) * g + 3) / 4 * 4;
     if (a->workspace_bytes < tree_bytes(hd, P.blocks, P.part_rows)) return SDV_ENOMEM;
     const size_t parts = (size_t)P.blocks * 2 * P.part_rows;
     uint8_t* ws = (uint8_t*)a->workspace;
     P.part_ml = (float2*)ws;
     P.part_o = (float*)(ws + align256(parts * sizeof(float2)));
-    P.q = a->q;
     P.out = a->out;
     P.v = pages->v;
     P.block_table = a->block_table;
@@ -242,8 +251,6 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     P.cu_rows = a->cu_rows;
     P.parent = a->parent;
     P.status = a->status;
-    P.q_row_stride = a->q_row_stride;
-    P.q_head_stride = a->q_head_stride;
     P.out_row_stride = a->out_row_stride;
     P.out_head_stride = a->out_head_stride;
     P.table_stride = a->table_stride;
@@ -254,16 +261,21 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     P.n_rows = a->n_rows;
     P.n_kv = pages->n_kv_heads;
     P.g = g;
+    P.chunk = chunk;
     P.table_width = a->table_width;
     P.page_size = pages->page_size;
     while ((1 << P.page_shift) < pages->page_size) ++P.page_shift;
     P.n_pages = pages->n_pages;
     P.scale_log2e = a->scale * 1.4426950408889634f;
     P.wait_limit_ns = 2000000000ull;
-    CUtensorMap map_k, map_v;
+    CUtensorMap map_q, map_k, map_v;
     const int box_keys = min(pages->page_size, kTreeKeys);
     if (!make_page_map(&map_k, pages->k, pages, box_keys) || !make_page_map(&map_v, pages->v, pages, box_keys)) return SDV_EINVAL;
-    const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, map_k, map_v, P);
+    // queries: head_dim x heads x rows; boxes of 64 elements of all heads of a group of `chunk` rows
+    const long long q_dims[3] = {hd, a->n_q_heads, a->n_rows}, q_strides[2] = {a->q_head_stride, a->q_row_stride};
+    const int q_box[3] = {64, g, chunk};
+    if (!make_map(&map_q, a->q, pages->dtype, 3, q_dims, q_strides, q_box)) return SDV_EINVAL;
+    const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, map_q, map_k, map_v, P);
     if (first != SDV_OK || P.blocks == 1) return first;   // one block does everything alone
     // Merge: units of four (row, head) pairs, of 16 columns where that leaves no more than three blocks an SM (see tree_merge_kernel); as many at a time for a block
     // as three blocks an SM need.

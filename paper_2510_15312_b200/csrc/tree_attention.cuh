@@ -24,14 +24,13 @@ struct TreeShape {
 };
 
 struct TreeParams : TreeLists {
-    const void* q;
     void* out;
     const void* v;                     // pool, for values that are not finite
     const int *block_table, *parent;
     float* part_o;                     // [2][block][part_rows / 4][HD / 8][4][8]: four rows' 32 bytes make a line, for the storing warp and for the merge
     float2* part_ml;                   // [2][block][part_rows] maximum (log2 units), sum
     int* status;
-    long long q_row_stride, q_head_stride, out_row_stride, out_head_stride, table_stride, page_stride, head_stride, token_stride;
+    long long out_row_stride, out_head_stride, table_stride, page_stride, head_stride, token_stride;
     int page_shift, n_pages, part_rows, blocks;
     float scale_log2e;
     unsigned long long wait_limit_ns;
@@ -83,6 +82,11 @@ struct TreeScan {
     }
 };
 
+__device__ __forceinline__ void tma_load_3d(void* smem_dst, const void* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(smem_u32(smem_dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+                 : "memory");
+}
 __device__ __forceinline__ void tma_load_4d(void* smem_dst, const void* map, int x, int y, int z, int w, uint64_t* bar) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                  ::"r"(smem_u32(smem_dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
@@ -160,13 +164,14 @@ __device__ __forceinline__ void tree_add_not_finite(const TreeParams& P, const T
 // by those who see them at the end.
 template <typename T, int HD>
 __global__ void __launch_bounds__(kTreeThreads, kTreeBlocksPerSm)
-tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TreeParams P) {
+tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                      const __grid_constant__ TreeParams P) {
     using S = TreeShape<HD>;
-    constexpr int KSTEPS = HD / 16, UNITS = HD / 8;
+    constexpr int KSTEPS = HD / 16;
     extern __shared__ __align__(1024) uint8_t tree_smem[];
     uint8_t *Qs = tree_smem, *ring = Qs + S::kQBytes;
     struct Ctl {
-        uint64_t full[S::kSlots], empty[S::kSlots], s_full[2], p_ready[2], pv_done[2], q_ready, drained;
+        uint64_t full[S::kSlots], empty[S::kSlots], s_full[2], p_ready[2], pv_done[2], q_ready, q_free, drained;
         unsigned long long bad[4];     // rows of the tree with values that are not finite, by item (modulo 4)
         uint32_t tmem_base;
         int abort_flag;
@@ -187,12 +192,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         }
         for (int i = 0; i < 4; ++i) ctl->bad[i] = 0;
         mbar_init(&ctl->drained, 1);
-        mbar_init(&ctl->q_ready, 4);
+        mbar_init(&ctl->q_ready, 1);
+        mbar_init(&ctl->q_free, 1);
         ctl->abort_flag = 0;
         mbar_fence_init();
     }
     if (warp == 5) tmem_alloc(&ctl->tmem_base, 256);   // S0 | S1, 64 columns each | O, HD columns
-    if (warp == 4 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &map_v : &map_k) : "memory");
+    if (warp == 4 && lane < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v) : "memory");
     grid_dep_wait();
     ctl->scan.fill(P);
     tc_fence_before();
@@ -270,7 +276,21 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             ok = ok && mbar_wait_bounded(bar, parity, &ctl->abort_flag, P.wait_limit_ns);
             ok = __all_sync(0xffffffffu, ok);
         };
-        const auto scores = [&]() {
+        // The queries of an item: all heads of the group of `chunk` rows, those of the next sequence behind its last row among them, which nobody looks at.
+        const auto load_q = [&](const TreeCursor& c) {
+            if (elect_one()) {
+                mbar_arrive_expect_tx(&ctl->q_ready, (uint32_t)(S::kAtoms * 128 * P.chunk * P.g));
+#pragma unroll
+                for (int a = 0; a < S::kAtoms; ++a) tma_load_3d(Qs + a * (kTreeTileRows * 128), &map_q, a * 64, c.h * P.g, c.s.first + c.c * P.chunk, &ctl->q_ready);
+            }
+            __syncwarp();
+        };
+        uint32_t q_loads = 0;
+        if (cur.left > 0) {
+            load_q(cur);
+            ++q_loads;
+        }
+        const auto scores = [&](bool last) {
             // the buffer held the probabilities of the tile two back: products into different accumulators are not ordered among themselves
             // (waited for is the newest product: within an item that of the tile two back)
             if (n_p > 0) wait(&ctl->pv_done[(n_p - 1u) & 1u], ((n_p - 1u) >> 1) & 1u);
@@ -285,6 +305,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                               umma_desc_sw128(k + (uint32_t)((ks >> 2) * (kTreeKeys * 128) + (ks & 3) * 32)), id_s, (uint32_t)ks);
                 umma_commit(&ctl->empty[s_k]);
                 umma_commit(&ctl->s_full[n_s & 1u]);
+                if (last) umma_commit(&ctl->q_free);
             }
             __syncwarp();
             ++n_s;
@@ -294,10 +315,18 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         uint32_t s_v = 1, par_v = 0;
         while (cur.left > 0 && ok) {
             const int n = cur.run();
+            TreeCursor nxt = cur;
+            nxt.skip(P, n);
             wait(&ctl->q_ready, item & 1u);
-            if (ok) scores();
+            if (ok) scores(n == 1);
             for (int j = 0; j < n && ok; ++j) {
-                if (j + 1 < n) scores();
+                if (j + 1 < n) scores(j + 2 == n);
+                if (j + 1 == n && nxt.left > 0) {   // the item's last scores are under way: the next item's queries take the place of this one's behind them
+                    wait(&ctl->q_free, item & 1u);
+                    if (!ok) break;
+                    load_q(nxt);
+                    ++q_loads;
+                }
                 wait(&ctl->full[s_v], par_v);
                 wait(&ctl->p_ready[n_p & 1u], (n_p >> 1) & 1u);
                 if (!ok) break;
@@ -317,8 +346,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 if (s_v >= S::kSlots) { s_v -= S::kSlots; par_v ^= 1u; }
             }
             ++item;
-            cur.skip(P, n);
+            cur = nxt;
         }
+        if (q_loads) mbar_drain(&ctl->q_ready, (q_loads - 1u) & 1u, P.wait_limit_ns);   // where a wait was given up, nobody else waits for the last copy
         if (!ok) {
             // behind an abandoned wait: tensor and shared memory are given back only when no product uses them any more
             if (elect_one()) umma_commit(&ctl->drained);
@@ -334,31 +364,12 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         int mask_b = -1;
         unsigned long long anc0 = 0, anc1 = 0;
         uint32_t v_slot = 1, v_par = 0;
-        // An item's query rows are copied asynchronously; tile rows without one keep what they hold.
-        const auto request_q = [&](const TreeCursor& c) {
-            const int r = c.c * kTreeTileRows + t, j = r / P.g, hh = r - j * P.g;
-            if (j < c.s.rows) {
-                const T* src = (const T*)P.q + (c.s.first + j) * P.q_row_stride + (c.h * P.g + hh) * P.q_head_stride;
-#pragma unroll
-                for (int i = 0; i < UNITS; ++i) cp_async_16_zfill(Qs + (i >> 3) * (kTreeTileRows * 128) + swz_unit(t, i & 7), src + i * 8, true);
-            }
-            cp_async_commit();
-        };
-        const auto announce_q = [&]() {
-            cp_async_wait<0>();
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl->q_ready);
-        };
-        if (cur.left > 0) {
-            request_q(cur);
-            announce_q();
-        }
         while (cur.left > 0) {
             const int n = cur.run();
             const TreeSeq& sq = cur.s;
-            const int r = cur.c * kTreeTileRows + t, j = r / P.g, hh = r - j * P.g;
-            const bool real = j < sq.rows, some = cur.c * kTreeTileRows + warp * 32 < sq.rows * P.g;   // this row, any row of the warp
+            const int jt = t / P.g, j = cur.c * P.chunk + jt, hh = t - jt * P.g;                       // row of the sequence, head of the group
+            const int rows_here = min(P.chunk, sq.rows - cur.c * P.chunk) * P.g;
+            const bool real = t < rows_here, some = warp * 32 < rows_here;                             // this row, any row of the warp
             unsigned long long see = j < 63 ? (2ull << j) - 1 : ~0ull;                                 // rows of the sequence this row sees
             if (P.parent) {
                 if (mask_b != cur.b) {
@@ -404,7 +415,6 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (k == n - 1 && nxt.left > 0) request_q(nxt);   // the item's last scores are there: its queries are not needed any more
                 if (some) {
                     tc_fence_after();
                     uint32_t v[2][32];
@@ -472,7 +482,6 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 v_slot += 2;
                 if (v_slot >= S::kSlots) { v_slot -= S::kSlots; v_par ^= 1u; }
             }
-            if (nxt.left > 0 && ok) announce_q();
             if (ok) ok = mbar_wait_bounded(&ctl->pv_done[(n_t - 1u) & 1u], ((n_t - 1u) >> 1) & 1u, &ctl->abort_flag, P.wait_limit_ns);
             ok = __all_sync(0xffffffffu, ok);
             const bool whole = n == sq.tiles;
@@ -596,16 +605,21 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, my_row = (lane >> 1) & 3;
     const bool fine = split * 16 == HD;
     const int place = fine ? lane & 15 : lane, few = fine ? 1 : kMergeFew;
-    // Rows of units are numbered by the (row, query head) pairs of a KV head in fours, those of a sequence beginning a new one.  (The host sees to it that
-    // the number of units stays within 32 bits.)
-    const auto first_unit = [&](int b) { return (int)((unsigned)(rows_begin(P.cu_rows, b, P.n_rows) * P.g + 3) / 4u) + b; };
+    // Units are numbered by the (row, query head) pairs of a KV head in fours, every sequence and every tile of rows beginning a new one: with n rows before it, a sequence
+    // begins behind ceil(n g / 4) fours, as many broken ones as there are sequences before it, and as many as whole tiles fit n.  (The host sees to it that the number of
+    // units stays within 32 bits.)
+    const auto first_unit = [&](int b) {
+        const unsigned first = rows_begin(P.cu_rows, b, P.n_rows);
+        return (int)((first * P.g + 3u) / 4u + first / P.chunk) + b;
+    };
+    const int chunk_units = (P.chunk * P.g + 3) / 4;
     const int per = TreeScan<kMergeWarps>::per(P);
     unit0[threadIdx.x] = (int)threadIdx.x * per < P.n_seqs ? first_unit((int)threadIdx.x * per) : INT_MAX;
     scan.fill(P);
     __syncthreads();
     const int total = scan.total(), cols = HD / split;
     const TreeCut cut(total, P.blocks);
-    const unsigned tasks = ((unsigned)(P.n_rows * P.g + 3) / 4u + P.n_seqs) * P.n_kv * split;
+    const unsigned tasks = ((unsigned)(P.n_rows * P.g + 3) / 4u + (unsigned)P.n_rows / P.chunk + P.n_seqs) * P.n_kv * split;
     bool waited = false;
     for (unsigned p0 = blockIdx.x; p0 < tasks; p0 += gridDim.x * group) {
         if (warp < group) {
@@ -627,17 +641,19 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
                 const int end = min(b + per, P.n_seqs) - 1;
                 while (b < end && first_unit(b + 1) <= unit) tile0 += tree_tiles(P, tree_seq(P, b++));
                 const TreeSeq s = tree_seq(P, b);
-                const int j0 = (unit - first_unit(b)) * 4;
-                if (j0 >= 0 && j0 < s.rows * P.g && s.tiles > 0) {
-                    q.first = s.first;
-                    q.j0 = j0;
-                    q.rows = min(4, s.rows * P.g - j0);
-                    const int c = j0 / kTreeTileRows;
-                    tile0 += (q.h * s.chunks + c) * s.tiles;
-                    q.block0 = cut.owner(tile0);
-                    q.n = cut.owner(tile0 + s.tiles - 1) - q.block0 + 1;
-                    q.row = j0 - c * kTreeTileRows;
-                    q.late = cut.begin(q.block0) < tile0;
+                const int u0 = unit - first_unit(b);
+                if (u0 >= 0 && u0 < s.chunks * chunk_units && s.tiles > 0) {
+                    const int c = u0 / chunk_units, rows = min(P.chunk, s.rows - c * P.chunk) * P.g;
+                    q.row = (u0 - c * chunk_units) * 4;
+                    if (q.row < rows) {
+                        q.first = s.first;
+                        q.j0 = c * P.chunk * P.g + q.row;
+                        q.rows = min(4, rows - q.row);
+                        tile0 += (q.h * s.chunks + c) * s.tiles;
+                        q.block0 = cut.owner(tile0);
+                        q.n = cut.owner(tile0 + s.tiles - 1) - q.block0 + 1;
+                        q.late = cut.begin(q.block0) < tile0;
+                    }
                 }
             }
             if (lane == 0) shared_unit[warp] = q;

@@ -23,12 +23,13 @@ template <typename T> inline T max(T a, T b) { return a < b ? b : a; }
 #endif
 
 constexpr int kTreeKeys = 64;          // keys of a tile
-constexpr int kTreeTileRows = 128;     // query rows of a tile: one query head of one row each
+constexpr int kTreeTileRows = 128;     // query rows of a tile: one query head of one row each, all heads of a group of as many rows as fit
 
 // The caller's index arrays and sizes.
 struct TreeLists {
     const int *kv_len, *cu_rows;
-    int n_seqs, n_rows, n_kv, g, table_width, page_size;   // g: query heads per KV head
+    int n_seqs, n_rows, n_kv, g, table_width, page_size;   // g: query heads per KV head (at most 128)
+    int chunk;                                             // rows of a tile: kTreeTileRows / g
 };
 
 // Rows of sequence b, whatever cu_rows holds: within [0, n_rows), none where the array descends.
@@ -38,7 +39,7 @@ SDV_HD int rows_count(const int* cu, int b, int n_rows) { return max(0, rows_beg
 // One sequence as the kernels see it, whatever the arrays hold.
 struct TreeSeq {
     int first, rows, length, keys;     // first row, rows, committed tokens, tokens in all (those the block table has room for)
-    int chunks, tiles;                 // tiles of 128 query rows (row, head of the group), tiles of keys
+    int chunks, tiles;                 // tiles of query rows, tiles of keys
 };
 SDV_HD TreeSeq tree_seq(const TreeLists& P, int b) {
     TreeSeq s;
@@ -47,7 +48,7 @@ SDV_HD TreeSeq tree_seq(const TreeLists& P, int b) {
     const long long room = min((long long)P.table_width * P.page_size, 0x7fffffffll - kTreeKeys);
     s.length = (int)min((long long)max(SDV_LD(P.kv_len + b), 0), room);
     s.keys = (int)min((long long)s.length + s.rows, room);
-    s.chunks = (s.rows * P.g + kTreeTileRows - 1) / kTreeTileRows;
+    s.chunks = (s.rows + P.chunk - 1) / P.chunk;
     s.tiles = s.rows ? (s.keys + kTreeKeys - 1) / kTreeKeys : 0;
     return s;
 }

@@ -74,7 +74,8 @@ int main() {
         TreeLists P;
         P.n_seqs = pick(1, round % 7 ? 12 : 200);
         P.n_kv = pick(1, 8);
-        P.g = pick(1, 9);
+        P.g = pick(0, 9) ? pick(1, 9) : pick(1, 128);
+        P.chunk = kTreeTileRows / P.g;
         P.page_size = 8 << pick(0, 4);
         P.table_width = pick(1, 40);
         std::vector<int> len, cu{0};
@@ -98,7 +99,7 @@ int main() {
     // lengths and tables at the ends of their types
     for (int len : {0x7fffffff, -1, 0x7fffffff - 63, 0}) {
         int cu[2] = {0, 9};
-        TreeLists P{&len, cu, 1, 9, 1, 1, 0x7fffffff, 1 << 20};
+        TreeLists P{&len, cu, 1, 9, 1, 1, 0x7fffffff, 1 << 20, kTreeTileRows};
         const TreeSeq s = tree_seq(P, 0);
         if (s.keys < s.length || s.keys < 0 || s.tiles < 1 || (long long)s.tiles * kTreeKeys < s.keys) return 2;
     }
