@@ -35,12 +35,12 @@ bool on_device(std::initializer_list<const void*> ps, int dev, size_t align) {
     return true;
 }
 
-int sm_count(int dev) {
+int sm_count(int dev) {   // 1 where it cannot be told
     static std::atomic<int> known[64];
-    if (dev < 0 || dev >= 64) return 0;
-    int n = known[dev].load(std::memory_order_relaxed);
-    if (!n && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) known[dev].store(n, std::memory_order_relaxed);
-    return n;
+    const bool keep = dev >= 0 && dev < 64;
+    int n = keep ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (!n && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && keep) known[dev].store(n, std::memory_order_relaxed);
+    return max(n, 1);
 }
 
 // A launch, in clusters of `cluster` blocks, that may overlap the tail of the kernel before it: each kernel waits for that one's end before it reads what it may have written.
@@ -289,6 +289,8 @@ int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {
     if (!a || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->vocab < 1 || a->vocab > kMaxVocab) return SDV_EINVAL;
     if ((a->draft && a->parent) || (!a->slots) != (!a->out_slots)) return SDV_EINVAL;
     if (a->target_stride < a->vocab || (a->draft && a->draft_stride < a->vocab)) return SDV_EINVAL;
+    // a sequence's blocks read what these hold while the first of them writes
+    if (a->out_tokens == a->tokens || a->out_rows == a->tokens || a->out_tokens == a->out_rows || (a->slots && (a->out_slots == a->slots || a->out_slots == a->tokens))) return SDV_EINVAL;
     if (a->n_seqs == 0 || a->n_rows == 0) return SDV_OK;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;

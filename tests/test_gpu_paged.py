@@ -389,5 +389,9 @@ def test_verify_refuses():
                   ((t, tok, cu, u), dict(draft_probs=t, parent=tok)), ((t, tok, cu, u), dict(draft_probs=t[:, :9])), ((t.cpu(), tok, cu, u), {}), ((t, tok, cu, u), dict(slots=tok[:3]))):
         with pytest.raises(ValueError):
             pkg.verify_sampled(*a, **kw)
+    out = [torch.zeros(n, dtype=torch.int32, device="cuda") for n in (1, 4, 4)] + [None]
+    for bad in ((t, tok, cu, u, dict(out=(out[0], tok, out[2], None))), (t[:1].expand(4, 10), tok, cu, u, {})):   # outputs over inputs, rows on top of each other
+        with pytest.raises(pkg.SdvError):
+            pkg.verify_sampled(*bad[:4], **bad[4])
     accepted, words, rows, slots = pkg.verify_sampled(t[:0], tok[:0], i32([0]), u[:0])
     assert accepted.numel() == 0 and words.numel() == 0 and slots is None

@@ -115,6 +115,24 @@ def test_attention_over_many_shares(rows, lengths, hq, hkv, hd):
     Case(rows, lengths, hq, hkv, hd, 32, "float16", True, seed=8).check(Case(rows, lengths, hq, hkv, hd, 32, "float16", True, seed=8).run())
 
 
+@pytest.mark.parametrize("hq,hkv,hd,rows", [(32, 1, 64, 9), (128, 1, 64, 3), (128, 2, 128, 5), (100, 1, 64, 2), (43, 1, 128, 40), (5, 5, 64, 64)])
+def test_groups_of_many_heads(hq, hkv, hd, rows):
+    """All heads of a group of as many rows as fit 128 tile rows: one row, two, all of them; tiles that stay partly empty."""
+    c = Case([rows, 1, rows], [90, 0, 333], hq, hkv, hd, 16, "float16", True, seed=hq)
+    c.check(c.run())
+
+
+def test_as_many_sequences_as_there_may_be():
+    c = Case([1] * 4096, [i % 7 for i in range(4096)], 2, 1, 64, 8, "bfloat16")
+    c.check(c.run(), only=range(0, 4096, 97))
+    import torch
+    d = Case([1] * 2000 + [30] + [1] * 2000, [3] * 2000 + [5000] + [i % 90 for i in range(2000)], 2, 1, 64, 32, "bfloat16")   # a long one among them
+    d.check(d.run(), only=[0, 1, 1999, 2000, 2001, 3999, 4000])
+    with pytest.raises(pkg.SdvError):
+        e = torch.zeros(4097, dtype=torch.int32, device="cuda")
+        pkg.tree_attention(c.q, c.k, c.v, e[:, None], e, torch.zeros(4098, dtype=torch.int32, device="cuda"))
+
+
 def test_maxima_that_keep_growing():
     """Keys sorted so that every tile brings larger scores: the output is rescaled again and again."""
     import torch
@@ -277,6 +295,74 @@ def test_streams_workspaces_and_graphs():
     c.lengths = [500, 3]
     g.replay()
     assert torch.equal(out[:39], c.run()[:39])
+
+
+def test_two_graphs_with_one_workspace():
+    """Replayed one after the other on one stream they may share it."""
+    import torch
+    a, b = Case([9], [3000], 12, 2, 128, 16, seed=1), Case([4, 4], [500, 1200], 12, 2, 128, 16, tree=True, seed=2)
+    want = [a.run(), b.run()]
+    ws = pkg.tree_attention_workspace(2, 128)
+    outs, graphs, held = [], [], []
+    for c in (a, b):
+        args = dict(block_table=i32(c.table), kv_len=i32(c.lengths), cu_rows=i32(c.cu), parent=None if c.parent is None else i32(c.parent))
+        out = torch.full_like(c.q, 77.0)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            pkg.tree_attention(c.q, c.k, c.v, out=out, workspace=ws, **args)
+        outs.append(out)
+        graphs.append(g)
+        held.append(args)
+    for order in ((0, 1), (1, 0), (0, 0), (1, 1)):
+        for k in order:
+            outs[k].fill_(77.0)
+            graphs[k].replay()
+        assert all(torch.equal(outs[k], want[k]) for k in order)
+
+
+def test_a_captured_step():
+    """All four operators in one graph, replayed on other inputs in the same buffers: as called one by one."""
+    import torch
+    rng = np.random.default_rng(4)
+    hq, hkv, hd, page, vocab, rows = 6, 2, 128, 16, 3000, [9, 5, 20]
+    cu, n = i32([0, 9, 14, 34]), 34
+    parent, f = i32(forest(rng, rows, 4)), torch.tensor(pkg.rope_frequencies(hd)[0], dtype=torch.float64, device="cuda")
+    kv, held, state, table = i32([200, 0, 90]), i32([13, 0, 6]), i32([0, 0]), torch.full((3, 30), -1, dtype=torch.int32, device="cuda")
+    pages = rng.permutation(60).astype(np.int32)
+    table[0, :13], table[2, :6] = i32(pages[:13]), i32(pages[13:19])
+    free = i32(pages[19:])
+    q, k, v = (torch.zeros(n, h, hd, dtype=torch.bfloat16, device="cuda") for h in (hq, hkv, hkv))
+    kp, vp = (torch.tensor(rng.standard_normal((60, hkv, page, hd)), device="cuda").bfloat16() for _ in range(2))
+    target, tokens, u = torch.zeros(n, vocab, device="cuda"), i32(np.zeros(n)), torch.zeros(n, device="cuda")
+
+    def fill(seed):
+        r = np.random.default_rng(seed)
+        for x in (q, k, v):
+            x.copy_(torch.tensor(r.standard_normal(tuple(x.shape))).bfloat16())
+        p = spread(r, n, vocab)
+        target.copy_(torch.tensor(p))
+        tokens.copy_(torch.tensor(p.argmax(1).astype(np.int32)).roll(1))
+        u.copy_(torch.tensor(r.random(n).astype(np.float32)))
+        kv.copy_(torch.tensor([200 - seed, 0, 90 + seed], dtype=torch.int32))
+
+    def step():
+        slots, pos, h, s = pkg.paged_slots(kv, cu, table, held, free, state, page, n, parent=parent)
+        qr = pkg.rope_append(pos, f, q=q, k=k, v=v, k_pages=kp, v_pages=vp, slots=slots)
+        out = pkg.tree_attention(qr, kp, vp, table, kv, cu, parent=parent)
+        return (slots, pos, h, s, qr, out) + tuple(pkg.verify_sampled(target, tokens, cu, u, parent=parent, slots=slots))
+
+    fill(0)
+    step()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    for seed in (1, 2, 3):
+        fill(seed)
+        want = [x.clone() for x in step()]
+        for x in got:
+            x.zero_()
+        g.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_attention_refuses():

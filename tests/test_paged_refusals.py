@@ -33,7 +33,7 @@ def good_attention(**kw):
 
 
 def good_verify(**kw):
-    f = dict(target=P, draft=None, tokens=P, cu_rows=P, parent=None, slots=None, uniforms=P, accept_len=P, out_tokens=P, out_rows=P, out_slots=None, target_stride=100,
+    f = dict(target=P, draft=None, tokens=P, cu_rows=P, parent=None, slots=None, uniforms=P, accept_len=P, out_tokens=2 * P, out_rows=3 * P, out_slots=None, target_stride=100,
              draft_stride=100, n_seqs=2, n_rows=5, vocab=100)
     return paged._VerifyArgs(**{**f, **kw})
 
@@ -68,13 +68,14 @@ def test_rope_refuses(kw):
 
 @pytest.mark.parametrize("kw", [dict(n_seqs=-1), dict(n_seqs=4097), dict(n_rows=-1), dict(n_q_heads=3), dict(n_q_heads=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf),
                                 dict(scale=math.nan), dict(table_stride=7), dict(q_row_stride=4), dict(q_head_stride=65), dict(out_row_stride=9), dict(out_head_stride=2),
-                                dict(table_width=-1), dict(pages=dict(head_dim=96)), dict(pages=dict(page_size=24)), dict(pages=dict(page_size=4)), dict(pages=dict(n_kv_heads=0))])
+                                dict(table_width=-1), dict(n_q_heads=258), dict(pages=dict(head_dim=96)), dict(pages=dict(page_size=24)), dict(pages=dict(page_size=4)), dict(pages=dict(n_kv_heads=0))])
 def test_attention_refuses(kw):
     assert attention(**kw) == pkg.EINVAL
 
 
 @pytest.mark.parametrize("kw", [dict(n_seqs=-1), dict(n_seqs=4097), dict(n_rows=-1), dict(vocab=0), dict(vocab=(1 << 21) + 1, target_stride=1 << 22), dict(target_stride=99),
-                                dict(draft=P, draft_stride=99), dict(draft=P, parent=P), dict(slots=P), dict(out_slots=P)])
+                                dict(draft=P, draft_stride=99), dict(draft=P, parent=P), dict(slots=P), dict(out_slots=P), dict(out_tokens=P), dict(out_rows=P), dict(out_rows=2 * P),
+                                dict(slots=5 * P, out_slots=5 * P), dict(slots=5 * P, out_slots=P)])
 def test_verify_refuses(kw):
     assert verify(**kw) == pkg.EINVAL
 
