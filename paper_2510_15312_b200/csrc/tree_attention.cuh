@@ -232,7 +232,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         };
         int page = cur.left > 0 ? page_of(cur, cur.tile) : -1;
         while (cur.left > 0 && ok) {
-            const int n = cur.run();
+            const int n = cur.run(P);
             TreeCursor nxt = cur;
             nxt.skip(P, n);
             for (int j = 0; j < n && ok; ++j) {
@@ -314,7 +314,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         };
         uint32_t s_v = 1, par_v = 0;
         while (cur.left > 0 && ok) {
-            const int n = cur.run();
+            const int n = cur.run(P);
             TreeCursor nxt = cur;
             nxt.skip(P, n);
             wait(&ctl->q_ready, item & 1u);
@@ -365,7 +365,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         unsigned long long anc0 = 0, anc1 = 0;
         uint32_t v_slot = 1, v_par = 0;
         while (cur.left > 0) {
-            const int n = cur.run();
+            const int n = cur.run(P);
             const TreeSeq& sq = cur.s;
             const int jt = t / P.g, j = cur.c * P.chunk + jt, hh = t - jt * P.g;                       // row of the sequence, head of the group
             const int rows_here = min(P.chunk, sq.rows - cur.c * P.chunk) * P.g;

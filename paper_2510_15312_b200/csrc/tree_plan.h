@@ -30,6 +30,7 @@ struct TreeLists {
     const int *kv_len, *cu_rows;
     int n_seqs, n_rows, n_kv, g, table_width, page_size;   // g: query heads per KV head (at most 128)
     int chunk;                                             // rows of a tile: kTreeTileRows / g
+    int whole;                                             // items (KV head, row chunk) are dealt out whole, not tile by tile
 };
 
 // Rows of sequence b, whatever cu_rows holds: within [0, n_rows), none where the array descends.
@@ -52,9 +53,10 @@ SDV_HD TreeSeq tree_seq(const TreeLists& P, int b) {
     s.tiles = s.rows ? (s.keys + kTreeKeys - 1) / kTreeKeys : 0;
     return s;
 }
-SDV_HD int tree_tiles(const TreeLists& P, const TreeSeq& s) { return s.tiles * s.chunks * P.n_kv; }
+// What a sequence adds to the list that is dealt out: tiles, or items.
+SDV_HD int tree_tiles(const TreeLists& P, const TreeSeq& s) { return (P.whole ? (s.tiles ? 1 : 0) : s.tiles) * s.chunks * P.n_kv; }
 
-// The tiles of all sequences, KV heads and row chunks in a row are cut into shares, one a block: the first blocks have one more than the last.  (The host refuses calls
+// The tiles (or items) of all sequences, KV heads and row chunks in a row are cut into shares, one a block: the first blocks have one more than the last.  (The host refuses calls
 // that could have 2^31 tiles.)
 struct TreeCut {
     int base, more;        // tiles of the last blocks, blocks with one more
@@ -71,23 +73,23 @@ struct TreeCut {
 
 // Cursor over a block's tiles: sequence, KV head, row chunk, key tile.
 struct TreeCursor {
-    int left;                          // tiles of the block still to do, this one included
+    int left;                          // tiles (items) of the block still to do, this one included
     int b, h, c, tile;
     TreeSeq s;
-    // n tiles from the offset-th of sequence b0 on (which has more than that)
+    // n tiles (items) from the offset-th of sequence b0 on (which has more than that)
     SDV_HD void start(const TreeLists& P, int b0, const TreeSeq& seq, int offset, int n) {
         left = n;
         b = b0;
         s = seq;
-        const int item = (int)((unsigned)offset / (unsigned)s.tiles);
-        tile = offset - item * s.tiles;
+        const int item = P.whole ? offset : (int)((unsigned)offset / (unsigned)s.tiles);
+        tile = P.whole ? 0 : offset - item * s.tiles;
         h = s.chunks == 1 ? item : (int)((unsigned)item / (unsigned)s.chunks);
         c = item - h * s.chunks;
     }
     // Tiles of the present item that belong to this block, from the present one on.
-    SDV_HD int run() const { return min(left, s.tiles - tile); }
+    SDV_HD int run(const TreeLists& P) const { return P.whole ? s.tiles : min(left, s.tiles - tile); }
     SDV_HD void skip(const TreeLists& P, int n) {   // n = run()
-        left -= n;
+        left -= P.whole ? 1 : n;
         if (left <= 0) return;
         tile = 0;
         if (++c < s.chunks) return;

@@ -24,7 +24,7 @@ static int check(const TreeLists& P, int blocks) {
         if (s.first < 0 || s.rows < 0 || s.first + s.rows > P.n_rows || s.rows > SDV_TREE_ROWS) return 1;
         if (s.length < 0 || s.keys < s.length || (long long)s.keys > (long long)P.table_width * P.page_size) return 2;
         if (s.keys - s.length > s.rows || (s.tiles > 0 && (s.tiles - 1) * kTreeKeys >= s.keys)) return 3;
-        before.push_back(before.back() + (long long)s.tiles * s.chunks * P.n_kv);
+        before.push_back(before.back() + (long long)(P.whole ? s.tiles > 0 : s.tiles) * s.chunks * P.n_kv);
     }
     if (before.back() > 0x3fffffffll) return 0;   // refused by the host
     const int total = (int)before.back();
@@ -43,14 +43,14 @@ static int check(const TreeLists& P, int blocks) {
         int item = 0;
         while (c.left > 0) {
             if (c.s.tiles == 0 || c.b >= P.n_seqs || c.h >= P.n_kv || c.c >= c.s.chunks || c.tile >= c.s.tiles) return 6;
-            const int n = c.run();
-            const long long at = before[c.b] + ((long long)c.h * c.s.chunks + c.c) * c.s.tiles + c.tile;
-            if (at != next) return 7;
-            for (int i = 0; i < n; ++i)
+            const int n = c.run(P), counted = P.whole ? 1 : n;
+            const long long at = before[c.b] + ((long long)c.h * c.s.chunks + c.c) * (P.whole ? 1 : c.s.tiles) + (P.whole ? 0 : c.tile);
+            if (at != next || (P.whole && (c.tile || n != c.s.tiles))) return 7;
+            for (int i = 0; i < counted; ++i)
                 if (cut.owner((int)at + i) != k) return 8;
             if (n != c.s.tiles) parts[{c.b, c.h, c.c}].push_back({k, item ? 1 : 0});
             if (n != c.s.tiles && item && c.left != n) return 9;   // a partial item that is not the block's first is its last
-            next += n;
+            next += counted;
             c.skip(P, n);
             ++item;
         }
@@ -76,6 +76,7 @@ int main() {
         P.n_kv = pick(1, 8);
         P.g = pick(0, 9) ? pick(1, 9) : pick(1, 128);
         P.chunk = kTreeTileRows / P.g;
+        P.whole = round % 4 == 3;
         P.page_size = 8 << pick(0, 4);
         P.table_width = pick(1, 40);
         std::vector<int> len, cu{0};
@@ -99,7 +100,7 @@ int main() {
     // lengths and tables at the ends of their types
     for (int len : {0x7fffffff, -1, 0x7fffffff - 63, 0}) {
         int cu[2] = {0, 9};
-        TreeLists P{&len, cu, 1, 9, 1, 1, 0x7fffffff, 1 << 20, kTreeTileRows};
+        TreeLists P{&len, cu, 1, 9, 1, 1, 0x7fffffff, 1 << 20, kTreeTileRows, 0};
         const TreeSeq s = tree_seq(P, 0);
         if (s.keys < s.length || s.keys < 0 || s.tiles < 1 || (long long)s.tiles * kTreeKeys < s.keys) return 2;
     }
