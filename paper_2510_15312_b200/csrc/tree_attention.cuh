@@ -105,6 +105,24 @@ template <typename T> __device__ __forceinline__ bool clear_not_finite(uint32_t&
     return lo || hi;
 }
 
+// Two fp32 numbers in a 64-bit register: one instruction for both.
+__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // Bit masks of the rows on the way from every row of a tree to its root, by doubling: lane l has rows l and l + 32.
 __device__ __forceinline__ void tree_masks(const TreeParams& P, const TreeSeq& s, int lane, unsigned long long& m0, unsigned long long& m1) {
     int p0 = lane, p1 = lane + 32;   // how far up the mask reaches: a row points at itself once it is at the root
@@ -434,7 +452,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     }
                     float m4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(v[i >> 5][i & 31]));
+                    for (int i = 0; i < 64; i += 2) m4[(i >> 1) & 3] = fmaxf(fmaxf(m4[(i >> 1) & 3], __uint_as_float(v[i >> 5][i & 31])), __uint_as_float(v[i >> 5][(i & 31) + 1]));
                     const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * P.scale_log2e;
                     const bool grow = real && mx > m + 8.f;   // also the first tile that shows this row a key
                     const bool rescale = grow && m != -CUDART_INF_F;
@@ -459,21 +477,27 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     }
                     if (grow) m = mx;
                     const float ref = m == -CUDART_INF_F ? 0.f : m;
-                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+                    const uint64_t sc2 = pack_f32x2(P.scale_log2e, P.scale_log2e), ref2 = pack_f32x2(-ref, -ref);
+                    uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         uint32_t pk[16];
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
-                            const float x = ex2_ftz(fmaf(__uint_as_float(v[c][i]), P.scale_log2e, -ref));
-                            const float y = ex2_ftz(fmaf(__uint_as_float(v[c][i + 1]), P.scale_log2e, -ref));
-                            s4[i & 2] += x;
-                            s4[(i & 2) + 1] += y;
+                            float x, y;
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1])), sc2, ref2), x, y);
+                            x = ex2_ftz(x);
+                            y = ex2_ftz(y);
+                            sum2[(i >> 1) & 1] = add_f32x2(sum2[(i >> 1) & 1], pack_f32x2(x, y));
                             pk[i / 2] = Half16<T>::pack(x, y);
                         }
                         tmem_st16(ts + 16u * (uint32_t)c, pk);   // over scores this thread has read
                     }
-                    l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    {
+                        float x, y;
+                        unpack_f32x2(add_f32x2(sum2[0], sum2[1]), x, y);
+                        l += x + y;
+                    }
                     tmem_st_wait();
                     tc_fence_before();
                 }
