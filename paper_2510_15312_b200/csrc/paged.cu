@@ -80,7 +80,7 @@ RopeKernel rope_kernel(int dtype, bool interleaved, bool wide) { return dtype ==
 typedef void (*RopeStaged)(const sdv_rope_args, const sdv_pages, int, int);
 RopeStaged rope_staged(int dtype) { return dtype == SDV_BF16 ? rope_staged_kernel<__nv_bfloat16> : rope_staged_kernel<__half>; }
 
-typedef void (*TreeKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const TreeParams);
+typedef void (*TreeKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const TreeParams);
 typedef void (*MergeKernel)(const TreeParams, int, int);
 TreeKernel tree_kernel(int dtype, int hd) {
     if (dtype == SDV_BF16) return hd == 128 ? tree_attention_kernel<__nv_bfloat16, 128> : tree_attention_kernel<__nv_bfloat16, 64>;
@@ -267,20 +267,21 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     P.n_kv = pages->n_kv_heads;
     P.g = g;
     P.chunk = chunk;
+    P.q_step = min(8, chunk);
     P.table_width = a->table_width;
     P.page_size = pages->page_size;
     while ((1 << P.page_shift) < pages->page_size) ++P.page_shift;
     P.n_pages = pages->n_pages;
     P.scale_log2e = a->scale * 1.4426950408889634f;
     P.wait_limit_ns = 2000000000ull;
-    CUtensorMap map_q, map_k, map_v;
+    CUtensorMap map_q, map_q1, map_k, map_v;
     const int box_keys = min(pages->page_size, kTreeKeys);
     if (!make_page_map(&map_k, pages->k, pages, box_keys) || !make_page_map(&map_v, pages->v, pages, box_keys)) return SDV_EINVAL;
-    // queries: head_dim x heads x rows; boxes of 64 elements of all heads of a group of `chunk` rows
+    // queries: head_dim x heads x rows; boxes of 64 elements of all heads of a group, of q_step rows and of one
     const long long q_dims[3] = {hd, a->n_q_heads, a->n_rows}, q_strides[2] = {a->q_head_stride, a->q_row_stride};
-    const int q_box[3] = {64, g, chunk};
-    if (!make_map(&map_q, a->q, pages->dtype, 3, q_dims, q_strides, q_box)) return SDV_EINVAL;
-    const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, map_q, map_k, map_v, P);
+    const int q_box[3] = {64, g, P.q_step}, q_box1[3] = {64, g, 1};
+    if (!make_map(&map_q, a->q, pages->dtype, 3, q_dims, q_strides, q_box) || !make_map(&map_q1, a->q, pages->dtype, 3, q_dims, q_strides, q_box1)) return SDV_EINVAL;
+    const int first = launch(tree_kernel(pages->dtype, hd), P.blocks, kTreeThreads, tree_smem(hd), cuda_stream, 1, map_q, map_q1, map_k, map_v, P);
     if (first != SDV_OK || P.whole || P.blocks == 1) return first;   // nothing is in parts
     // Merge: units of four (row, head) pairs, of 16 columns where that leaves no more than three blocks an SM (see tree_merge_kernel); as many at a time for a block
     // as three blocks an SM need.

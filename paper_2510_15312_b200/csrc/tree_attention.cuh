@@ -31,7 +31,7 @@ struct TreeParams : TreeLists {
     float2* part_ml;                   // [2][block][part_rows] maximum (log2 units), sum
     int* status;
     long long out_row_stride, out_head_stride, table_stride, page_stride, head_stride, token_stride;
-    int page_shift, n_pages, part_rows, blocks;
+    int page_shift, n_pages, part_rows, blocks, q_step;
     float scale_log2e;
     unsigned long long wait_limit_ns;
 };
@@ -182,7 +182,7 @@ __device__ __forceinline__ void tree_add_not_finite(const TreeParams& P, const T
 // by those who see them at the end.
 template <typename T, int HD>
 __global__ void __launch_bounds__(kTreeThreads, kTreeBlocksPerSm)
-tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_q1, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                       const __grid_constant__ TreeParams P) {
     using S = TreeShape<HD>;
     constexpr int KSTEPS = HD / 16;
@@ -215,8 +215,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         ctl->abort_flag = 0;
         mbar_fence_init();
     }
+    for (int i = tid; i < S::kQBytes / 16; i += kTreeThreads) reinterpret_cast<uint4*>(Qs)[i] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
     if (warp == 5) tmem_alloc(&ctl->tmem_base, 256);   // S0 | S1, 64 columns each | O, HD columns
-    if (warp == 4 && lane < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v) : "memory");
+    if (warp == 4 && lane < 4) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_q1 : lane == 2 ? &map_k : &map_v) : "memory");
     grid_dep_wait();
     ctl->scan.fill(P);
     tc_fence_before();
@@ -294,12 +296,19 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             ok = ok && mbar_wait_bounded(bar, parity, &ctl->abort_flag, P.wait_limit_ns);
             ok = __all_sync(0xffffffffu, ok);
         };
-        // The queries of an item: all heads of the group of `chunk` rows, those of the next sequence behind its last row among them, which nobody looks at.
+        // The queries of an item, all heads of the group: `q_step` rows a copy, the last ones one by one.  Other tile rows keep what they hold, zeros to begin with: products with
+        // them cost power (a long run over 64 sequences of one row took 121 us a call with the neighbours' queries in them, 114 with zeros).
         const auto load_q = [&](const TreeCursor& c) {
             if (elect_one()) {
-                mbar_arrive_expect_tx(&ctl->q_ready, (uint32_t)(S::kAtoms * 128 * P.chunk * P.g));
+                const int rows = min(P.chunk, c.s.rows - c.c * P.chunk), row0 = c.s.first + c.c * P.chunk;
+                mbar_arrive_expect_tx(&ctl->q_ready, (uint32_t)(S::kAtoms * 128 * rows * P.g));
+                for (int r = 0; r < rows;) {
+                    const bool many = rows - r >= P.q_step;
 #pragma unroll
-                for (int a = 0; a < S::kAtoms; ++a) tma_load_3d(Qs + a * (kTreeTileRows * 128), &map_q, a * 64, c.h * P.g, c.s.first + c.c * P.chunk, &ctl->q_ready);
+                    for (int a = 0; a < S::kAtoms; ++a)
+                        tma_load_3d(Qs + a * (kTreeTileRows * 128) + r * P.g * 128, many ? &map_q : &map_q1, a * 64, c.h * P.g, row0 + r, &ctl->q_ready);
+                    r += many ? P.q_step : 1;
+                }
             }
             __syncwarp();
         };
@@ -397,7 +406,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 const unsigned long long a0 = __shfl_sync(0xffffffffu, anc0, j & 31), a1 = __shfl_sync(0xffffffffu, anc1, j & 31);
                 see = j < 32 ? a0 : a1;
             }
-            float m = -CUDART_INF_F, l = 0.f;
+            float m = real ? -CUDART_INF_F : CUDART_INF_F, l = 0.f;   // (the probabilities of a tile row without a query are zeros)
             TreeCursor nxt = cur;
             nxt.skip(P, n);
             for (int k = 0; k < n; ++k, ++n_t) {
