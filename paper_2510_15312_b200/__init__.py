@@ -1,7 +1,8 @@
 """sdv: the verify path of retrieval-based greedy speculative decoding on one B200.
 
 Python binding of the C-ABI library declared in include/sdv.h: argument marshalling only,
-every step of the path runs in the library's CUDA kernels.  PyTorch is used for device memory
+every step of the path runs in the library's CUDA kernels.  Beside the contexts (Sdv) stand operators on plain device
+tensors: gemm_noalloc, and those on a cache kept in pages (paged.py).  PyTorch is used for device memory
 and streams.  There is no CPU fallback: importing works without a GPU, creating a context
 does not.
 """

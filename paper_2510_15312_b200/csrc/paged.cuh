@@ -24,8 +24,8 @@ __device__ __forceinline__ int last_not_above(const int* a, int n, int x) {
 constexpr int kSlotThreads = 512;
 
 // Every block sums up all sequences' needs (they are few: at most 4096) and takes its share of the rows and of the new table entries, which find their
-// sequence by bisection in shared memory: one launch and no block waits for another.  Bound by latency (launch, one round trip to
-// memory for the lengths, one for the tables).
+// sequence by bisection in shared memory: one launch and no block waits for another.  Bound by latency: launch, a round trip to
+// memory for the lengths, one for the tables (4.4 us for 5 sequences of 20 rows, 5.4 for 1000 of up to 47 rows and 33298 pages).
 struct SlotShared {
     int row0[SDV_MAX_SEQUENCES + 1];   // first row of every sequence
     int need0[SDV_MAX_SEQUENCES + 1];  // pages needed by the sequences before

@@ -169,14 +169,17 @@ __device__ __forceinline__ void tree_add_not_finite(const TreeParams& P, const T
     }
 }
 
-// All tiles of 64 keys of all sequences, KV heads and chunks of 128 query rows (a tile row is one query head of one row; the heads that share a KV head
-// and the rows of a sequence read the keys together) are one list, cut into equal shares over two blocks per SM, whatever the lengths: a block works through
-// parts of one or of many items, and what it did not do alone is merged by tree_merge_kernel from un-normalised outputs, maxima and sums in the workspace.
-// Within a block: keys and values come page by page through a ring of tensor-map copies; S = Q K^T goes to one of two tensor-memory buffers, is turned into
-// probabilities in place (a row per thread, no exchange between threads) and P V adds up in tensor memory, where it is rescaled only when a row's maximum grew by
-// more than 2^8 (the published FlashAttention-4 rule: probabilities stay below 2^8, sums are fp32).  S of the next tile is computed during
-// the softmax of this one.  A step over a long cache is bound by memory: 128 rows cost 0.35 us of tensor work and 0.3 us of exponentials
-// per tile of 64 keys and SM where the copies take 0.75 us.
+// out = sum_t softmax(scale q k_t) v_t with running maxima and sums.  A tile is 64 keys by up to 128 tile rows (a tile row is one query head of one row; the rows of a
+// sequence and the heads that share a KV head read the keys together).  All tiles of all sequences, KV heads and tiles of rows are one list, cut into equal shares
+// over two blocks an SM whatever the lengths: a block works through parts of one or of many items, and what it did not do alone is merged by tree_merge_kernel from
+// un-normalised outputs, maxima and sums in the workspace.  (Short tables are dealt out in whole items instead, see the host.)
+// Within a block: one warp copies keys and values, box by box of a page, into a ring of tiles (tensor maps: any strides, five tiles of 16 KB in flight a block); one issues S = Q K^T
+// into one of two tensor-memory buffers and, when four warps have turned it into probabilities in place (a tile row a thread, no exchange between threads), P V, which adds up in
+// tensor memory.  The output is rescaled only when a row's maximum grew by more than 2^8: probabilities stay below 2^8 and their sums, in fp32, lose nothing.  S of the next tile is
+// computed during the softmax of this one.  Probabilities are rounded to the 16-bit type for the second product, as its operand has to be; sums take them unrounded.
+// Bound by memory where the cache is long: 64 sequences of one row over up to 8192 tokens (619 MB, 7 heads a KV head) take 97 us here and 104 with the merge, 5.9 TB/s; a run of
+// many seconds is bound by power, 113 us.  24 trees of up to 40 rows (244 MB) take 49 us: 37 for the bytes, 4 until the first scores, the rest until the slowest block is through
+// (blocks of equal shares end up to 15 percent apart).  512 tile rows a KV head are bound by the L2, where each tile of rows reads the keys again.
 // Places behind a sequence's end hold anything: their values are cleared in shared memory (0 x NaN is not 0).  Rows of the tree
 // that a row does not see take part in its product with probability 0: infinities and NaN among their values are cleared too, and added
 // by those who see them at the end.
@@ -567,7 +570,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 // item, or 16 columns of them where there are so few units that each has a block; a lane has four columns of one row.  A warp takes a unit; those with more than
 // twelve parts, and the fine ones, are gone through by whole blocks (a long cache of few sequences is cut into up to 150 parts).  Neighbouring units are in different blocks, so that a long
 // sequence among short ones has many blocks' help.  Where the parts are follows from the lengths alone and is worked out before the attention is waited for.
-// Bound by latency: launch, a round trip to L2 for five parts, the store.
+// Bound by latency: 1.2 us behind the attention's last block, then a round trip to L2 of about 1 us for every two parts and 64 columns (alone) or five parts (together), the store:
+// 2.5 to 5 us in all.  (Loops are kept short: unrolled further, instruction fetches and spilled registers took more than they saved.)
 constexpr int kMergeWarps = 8, kMergeThreads = kMergeWarps * 32, kMergeDeep = 5 /* parts a warp has in flight */, kMergeFew = 12;
 struct TreeUnit {
     int block0, n;        // first block with a part, parts
