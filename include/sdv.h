@@ -447,7 +447,8 @@ int sdv_gemm_noalloc(const float *dev_x, const uint16_t *dev_w, float *dev_y, in
 enum { SDV_BF16 = 0, SDV_FP16 = 1 };
 
 /* Keys and values of one layer in pages: element d of token t of KV head h of page p at k[p * page_stride + h * head_stride +
- * t * token_stride + d] (strides in elements; the same for v).  Both 16-byte aligned, strides multiples of 8. */
+ * t * token_stride + d] (strides in elements; the same for v).  Both 16-byte aligned, strides multiples of 8 and positive where there is more
+ * than one of the thing; at most 2^31 - 1 tokens in all. */
 typedef struct {
     void *k, *v;
     int dtype;   /* SDV_BF16 or SDV_FP16 */
@@ -491,7 +492,8 @@ int sdv_rope_append(const sdv_rope_args *a, const sdv_pages *pages /* NULL witho
 
 /* Attention of every row over tokens [0, kv_len[b]) of its sequence and over the tokens of the rows on its own path (itself included),
  * which have been appended before: out = softmax(scale * q k^T) v, query head h with KV head h / (n_q_heads / n_kv_heads).  head_dim 64 or
- * 128, page_size a power of two from 8 on, scale > 0.  Scores, statistics and sums in fp32, probabilities rounded to the 16-bit
+ * 128, up to 128 query heads per KV head, page_size a power of two from 8 on, scale > 0, rows of q and out 16-byte aligned with strides of positive multiples of 8,
+ * at most 2^30 tiles of 64 keys.  Scores, statistics and sums in fp32, probabilities rounded to the 16-bit
  * type for the second product.  What lies in places that a row may not see, infinities and NaN too, does not reach it.  Tokens past
  * table_width * page_size are left out; entries of block_table outside the pool read as zeros.  Rows of a sequence past
  * SDV_TREE_ROWS and rows of no sequence are left as they were in `out`.  `workspace`: sdv_tree_attention_workspace_bytes bytes, 256-byte
@@ -523,7 +525,8 @@ int sdv_tree_attention(const sdv_attention_args *a, const sdv_pages *pages, void
  * rejected.  Out: accept_len[b] (-1: no rows); out_tokens, from entry cu_rows[b] on, the accept_len[b] accepted tokens and the drawn one; out_rows
  * likewise row 0 and the accepted rows, counted from row 0; -1 behind them and for rows of no sequence.  With slots (each row's, from sdv_paged_slots):
  * out_slots[r], where an accepted row's keys and values belong once the others are dropped, -1 for rows that are dropped or lie
- * there already.  Rows past SDV_TREE_ROWS are not looked at.  Probabilities are fp32; row strides in elements. */
+ * there already.  Rows past SDV_TREE_ROWS are not looked at.  Probabilities are fp32, vocab at most 2^21, row strides in
+ * elements.  Out arrays must not be in arrays. */
 typedef struct {
     const float *target, *draft;
     const int32_t *tokens, *cu_rows, *parent, *slots;

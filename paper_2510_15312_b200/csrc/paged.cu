@@ -64,9 +64,13 @@ int launch(void (*kernel)(KArgs...), int grid, int block, size_t smem, void* str
     return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? SDV_OK : SDV_ECUDA;
 }
 
+// An output's rows (or heads) do not lie on top of each other.
+bool spread(int n, long long stride) { return n <= 1 || stride > 0; }
+
 bool pages_ok(const sdv_pages* p, int dev) {
     if (!p || (p->dtype != SDV_BF16 && p->dtype != SDV_FP16)) return false;
     if (p->n_pages < 1 || p->page_size < 1 || p->n_kv_heads < 1 || p->head_dim < 1 || (long long)p->n_pages * p->page_size > INT_MAX) return false;
+    if (!spread(p->n_pages, p->page_stride) || !spread(p->n_kv_heads, p->head_stride) || !spread(p->page_size, p->token_stride)) return false;
     if (p->page_stride < 0 || p->head_stride < 0 || p->token_stride < 0 || ((p->page_stride | p->head_stride | p->token_stride) & 7)) return false;
     return on_device(p->k, dev, 16) && on_device(p->v, dev, 16);
 }
@@ -124,7 +128,8 @@ bool make_map(CUtensorMap* m, const void* base, int dtype, int rank, const long 
         d[i] = (cuuint64_t)dims[i];
         b[i] = (cuuint32_t)box[i];
         one[i] = 1;
-        if (i) s[i - 1] = (cuuint64_t)(dims[i] > 1 && strides[i - 1] ? strides[i - 1] * 2 : 16);   // of a dimension of one: anything valid
+        if (i && dims[i] > 1 && strides[i - 1] <= 0) return false;   // (rows on top of each other are not known to the copies)
+        if (i) s[i - 1] = (cuuint64_t)(dims[i] > 1 ? strides[i - 1] * 2 : 16);   // of a dimension of one: anything valid
     }
     return fn(m, dtype == SDV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, s, b, one,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -172,6 +177,7 @@ int sdv_rope_append(const sdv_rope_args* a, const sdv_pages* pages, void* cuda_s
     if (!a || a->n_rows < 0 || (a->dtype != SDV_BF16 && a->dtype != SDV_FP16)) return SDV_EINVAL;
     if (a->head_dim < 2 || a->head_dim > 256 || a->head_dim % 2 || a->rot_dim < 2 || a->rot_dim > a->head_dim || a->rot_dim % 2) return SDV_EINVAL;
     if ((!a->k) != (!a->v) || (!a->q && !a->k) || (a->q && a->n_q_heads < 1) || (a->k && a->n_kv_heads < 1)) return SDV_EINVAL;
+    if (a->q && (!spread(a->n_rows, a->out_row_stride) || !spread(a->n_q_heads, a->out_head_stride))) return SDV_EINVAL;
     if (a->n_rows == 0) return SDV_OK;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;
@@ -220,6 +226,7 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     if (a->n_q_heads < 1 || a->n_q_heads % pages->n_kv_heads || a->n_q_heads / pages->n_kv_heads > kTreeTileRows || !(a->scale > 0.f) || !isfinite(a->scale)) return SDV_EINVAL;
     if (a->table_stride < a->table_width && a->n_seqs > 1) return SDV_EINVAL;
     if ((a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride) & 7) return SDV_EINVAL;
+    if (!spread(a->n_rows, a->out_row_stride) || !spread(a->n_q_heads, a->out_head_stride)) return SDV_EINVAL;
     if (a->n_seqs == 0 || a->n_rows == 0 || a->table_width == 0) return SDV_OK;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;

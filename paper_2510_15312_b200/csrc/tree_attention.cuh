@@ -540,17 +540,17 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         for (int i = 0; i < 32; ++i) o[i] = 0x7fc00000u;   // NaN
                     }
                     if (real && ok && bad) tree_add_not_finite<T>(P, cur, bad, c, o);
-                    if (!real) continue;
-                    if (whole) {
+                    if (real && whole) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8)
                             *reinterpret_cast<uint4*>(dst + c + i) =
                                 make_uint4(Half16<T>::pack(__uint_as_float(o[i]) * sc, __uint_as_float(o[i + 1]) * sc), Half16<T>::pack(__uint_as_float(o[i + 2]) * sc, __uint_as_float(o[i + 3]) * sc),
                                            Half16<T>::pack(__uint_as_float(o[i + 4]) * sc, __uint_as_float(o[i + 5]) * sc), Half16<T>::pack(__uint_as_float(o[i + 6]) * sc, __uint_as_float(o[i + 7]) * sc));
-                    } else {
+                    } else if (real) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) st_global_v8(po + (c + i) * 4, o + i);
                     }
+                    __syncwarp();   // tensor memory is read by whole warps
                 }
                 tc_fence_before();
             }

@@ -374,7 +374,8 @@ def test_attention_refuses():
                 dict(kv_len=i32([20]).cpu()), dict(parent=i32([0])), dict(out=c.q.half()), dict(out=c.q[:1]), dict(k_pages=c.k.float(), v_pages=c.v.float(), q=c.q.float())):
         with pytest.raises(ValueError):
             pkg.tree_attention(**{**a, **bad})
-    for bad in (dict(scale=0.0), dict(scale=float("nan")), dict(workspace=torch.empty(1 << 10, dtype=torch.uint8, device="cuda")), dict(q=c.q[:, :3]), dict(q=c.q.view(-1)[4:4 + 4 * 64].view(1, 4, 64)),
+    for bad in (dict(q=c.q[:, :1].expand(c.n, 4, 64)), dict(q=c.q[:1].expand(c.n, 4, 64)), dict(out=torch.empty(c.n, 1, 64, dtype=c.t, device="cuda").expand(c.n, 4, 64)),
+                dict(k_pages=c.k[:, :1].expand_as(c.k), v_pages=c.v[:, :1].expand_as(c.v)), dict(scale=0.0), dict(scale=float("nan")), dict(workspace=torch.empty(1 << 10, dtype=torch.uint8, device="cuda")), dict(q=c.q[:, :3]), dict(q=c.q.view(-1)[4:4 + 4 * 64].view(1, 4, 64)),
                 dict(out=torch.empty(c.n * 256 + 1, dtype=c.t, device="cuda")[1:].view(c.n, 4, 64))):
         with pytest.raises(pkg.SdvError):
             pkg.tree_attention(**{**a, **bad})

@@ -61,14 +61,14 @@ def test_slots_refuses(kw):
 
 
 @pytest.mark.parametrize("kw", [dict(n_rows=-1), dict(dtype=2), dict(head_dim=63), dict(head_dim=258, rot_dim=64), dict(rot_dim=0), dict(rot_dim=66), dict(rot_dim=7), dict(k=None),
-                                dict(v=None), dict(q=None, k=None, v=None), dict(n_q_heads=0), dict(n_kv_heads=0)])
+                                dict(v=None), dict(q=None, k=None, v=None), dict(n_q_heads=0), dict(n_kv_heads=0), dict(out_row_stride=0), dict(out_head_stride=-64)])
 def test_rope_refuses(kw):
     assert rope(**kw) == pkg.EINVAL
 
 
 @pytest.mark.parametrize("kw", [dict(n_seqs=-1), dict(n_seqs=4097), dict(n_rows=-1), dict(n_q_heads=3), dict(n_q_heads=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf),
                                 dict(scale=math.nan), dict(table_stride=7), dict(q_row_stride=4), dict(q_head_stride=65), dict(out_row_stride=9), dict(out_head_stride=2),
-                                dict(table_width=-1), dict(n_q_heads=258), dict(pages=dict(head_dim=96)), dict(pages=dict(page_size=24)), dict(pages=dict(page_size=4)), dict(pages=dict(n_kv_heads=0))])
+                                dict(table_width=-1), dict(out_row_stride=0), dict(out_head_stride=0), dict(n_q_heads=258), dict(pages=dict(head_dim=96)), dict(pages=dict(page_size=24)), dict(pages=dict(page_size=4)), dict(pages=dict(n_kv_heads=0))])
 def test_attention_refuses(kw):
     assert attention(**kw) == pkg.EINVAL
 
