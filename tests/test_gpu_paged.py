@@ -395,3 +395,87 @@ def test_verify_refuses():
             pkg.verify_sampled(*bad[:4], **bad[4])
     accepted, words, rows, slots = pkg.verify_sampled(t[:0], tok[:0], i32([0]), u[:0])
     assert accepted.numel() == 0 and words.numel() == 0 and slots is None
+
+
+# ------------------------------------------------------------------------------------------ the calls themselves
+def calls():
+    """A call of each operator (without the stream) and the tensors it is given."""
+    import torch
+    q, k, v, kp, vp, pos, slot = rope_case("bfloat16", 6, 4, 2, 64, 64, False, 8, False, qkv=False)
+    f, t = torch.tensor(pkg.rope_frequencies(64)[0], dtype=torch.float64, device="cuda"), torch.rand(6, 10, device="cuda")
+    pos, slot, u, cu, length, tok = i32(pos), i32(slot), torch.rand(6, device="cuda"), i32([0, 6]), i32([2]), i32([0, 1, 2, 3, 4, 5])
+    table, held, free, state = i32([[0, 1, 2, 3]]), i32([1]), i32([1, 2, 3]), i32([0])
+    return [("paged_slots", (length, cu, table, held, free, state, 8, 6), {}),
+            ("rope_append", (pos, f, q, k, v, kp, vp, slot), {}),
+            ("rope_append", (pos, f), dict(k=k, v=v, k_pages=kp, v_pages=vp, slots=slot)),
+            ("tree_attention", (q, kp, vp, table, length, cu), {}),
+            ("verify_sampled", (t, tok, cu, u), {}),
+            ("verify_sampled", (t, tok, cu, u), dict(draft_probs=t, slots=slot))]
+
+
+def test_calls_keep_no_references():
+    """Neither the arguments nor the results outlive a call, refused or not."""
+    import sys
+    import torch
+    for name, a, kw in calls():
+        given = [x for x in (*a, *kw.values()) if torch.is_tensor(x)]
+        count = lambda: [sys.getrefcount(x) for x in given] + [sys.getrefcount(None)]  # noqa: E731
+        getattr(pkg, name)(*a, **kw)
+        torch.cuda.synchronize()
+        before, memory = count(), torch.cuda.memory_allocated()
+        for _ in range(50):
+            r = getattr(pkg, name)(*a, **kw)
+            with pytest.raises(ValueError):
+                getattr(pkg, name)(a[0][:, None], *a[1:], **kw)
+        del r
+        after = count()
+        assert after[:-1] == before[:-1] and abs(after[-1] - before[-1]) < 25 and torch.cuda.memory_allocated() == memory, name   # None's own count moves a little by itself
+
+
+def test_calls_refuse_what_is_no_tensor():
+    for name, a, kw in calls():
+        for i in range(len(a)):
+            if not isinstance(a[i], int):
+                with pytest.raises(ValueError):
+                    getattr(pkg, name)(*a[:i], "no tensor", *a[i + 1:], **kw)
+    name, a, kw = calls()[0]
+    for out in ((), (a[0],) * 3, (a[0],) * 5, (None,) * 4):
+        with pytest.raises(ValueError):
+            pkg.paged_slots(*a, out=out)
+    for bad in ((*a[:6], 8, -1), (*a[:7], 2 ** 40)):
+        with pytest.raises(ValueError):
+            pkg.paged_slots(*bad)
+    for size in (0, -8, 2 ** 40):
+        with pytest.raises(pkg.SdvError):
+            pkg.paged_slots(*a[:6], size, 6)
+    with pytest.raises(ValueError):
+        pkg.verify_sampled(*calls()[4][1], out=(a[0], a[0]))
+
+
+def test_calls_from_several_threads():
+    """Each thread has its own current stream; the answers are those of one thread."""
+    import threading
+    import torch
+    todo = calls()[3:]
+    want = [getattr(pkg, n)(*a, **kw) for n, a, kw in todo]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work():
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(100):
+                    got = [getattr(pkg, n)(*a, **kw) for n, a, kw in todo]
+                torch.cuda.current_stream().synchronize()
+            same = lambda x, y: torch.equal(x, y) if torch.is_tensor(x) else x is y  # noqa: E731
+            for g, w in zip(got, want):
+                if not all(same(x, y) for x, y in zip(g, w)):
+                    wrong.append(g)
+        except Exception as e:   # seen by the test, not by the thread
+            wrong.append(e)
+    threads = [threading.Thread(target=work) for _ in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong

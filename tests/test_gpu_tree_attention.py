@@ -384,10 +384,11 @@ def test_attention_refuses():
     assert e.value.code == pkg.ENOMEM
     host = torch.empty(1 << 12, dtype=torch.uint8).pin_memory()
     import ctypes as C
-    from paper_2510_15312_b200 import paged
-    pages = paged._Pages(*paged._pool(c.k, c.v, torch.cuda.current_device()))
-    args = paged._AttentionArgs(q=host.data_ptr() + 256 - host.data_ptr() % 256, out=c.q.data_ptr(), block_table=a["block_table"].data_ptr(), kv_len=a["kv_len"].data_ptr(),
-                                cu_rows=a["cu_rows"].data_ptr(), workspace=c.q.data_ptr(), workspace_bytes=1 << 30, table_stride=8, n_seqs=1, n_rows=2, n_q_heads=4, table_width=2, scale=1.0)
+    from paged_structs import AttentionArgs, Pages
+    pages = Pages(c.k.data_ptr(), c.v.data_ptr(), 0, c.k.shape[0], 16, 2, 64, *c.k.stride()[:3])
+    args = AttentionArgs(q=host.data_ptr() + 256 - host.data_ptr() % 256, out=c.q.data_ptr(), block_table=a["block_table"].data_ptr(), kv_len=a["kv_len"].data_ptr(),
+                         cu_rows=a["cu_rows"].data_ptr(), workspace=c.q.data_ptr(), workspace_bytes=1 << 30, q_row_stride=256, q_head_stride=64, out_row_stride=256, out_head_stride=64,
+                         table_stride=8, n_seqs=1, n_rows=2, n_q_heads=4, table_width=2, scale=1.0)
     assert pkg.lib().sdv_tree_attention(C.byref(args), C.byref(pages), None) == pkg.EINVAL     # host memory
     with pytest.raises(pkg.SdvError):
         pkg.tree_attention_workspace(5000, 64)

@@ -4,38 +4,38 @@ import math
 
 import pytest
 
+import paged_structs as paged
 import paper_2510_15312_b200 as pkg
-from paper_2510_15312_b200 import paged
 
 P = 256   # an address that is never read here
 
 
 def good_pages(**kw):
-    return paged._Pages(**{**dict(k=P, v=P, dtype=0, n_pages=4, page_size=16, n_kv_heads=2, head_dim=64, page_stride=2048, head_stride=1024, token_stride=64), **kw})
+    return paged.Pages(**{**dict(k=P, v=P, dtype=0, n_pages=4, page_size=16, n_kv_heads=2, head_dim=64, page_stride=2048, head_stride=1024, token_stride=64), **kw})
 
 
 def good_slots(**kw):
     f = dict(kv_len=P, cu_rows=P, parent=None, n_held=P, free_pages=P, free_state=P, block_table=P, slots=P, positions=P, n_held_out=2 * P, free_state_out=2 * P,
              table_stride=8, n_seqs=2, n_rows=5, page_size=16, table_width=8, n_free=9)
-    return paged._SlotsArgs(**{**f, **kw})
+    return paged.SlotsArgs(**{**f, **kw})
 
 
 def good_rope(**kw):
     f = dict(q=P, k=P, v=P, q_out=P, positions=P, slots=P, frequencies=P, q_row_stride=256, q_head_stride=64, out_row_stride=256, out_head_stride=64, k_row_stride=128,
              k_head_stride=64, v_row_stride=128, v_head_stride=64, n_rows=5, n_q_heads=4, n_kv_heads=2, head_dim=64, rot_dim=64, interleaved=0, dtype=0, factor=1.0)
-    return paged._RopeArgs(**{**f, **kw})
+    return paged.RopeArgs(**{**f, **kw})
 
 
 def good_attention(**kw):
     f = dict(q=P, out=P, block_table=P, kv_len=P, cu_rows=P, parent=None, workspace=P, status=None, workspace_bytes=1 << 30, q_row_stride=256, q_head_stride=64,
              out_row_stride=256, out_head_stride=64, table_stride=8, n_seqs=2, n_rows=5, n_q_heads=4, table_width=8, scale=0.125)
-    return paged._AttentionArgs(**{**f, **kw})
+    return paged.AttentionArgs(**{**f, **kw})
 
 
 def good_verify(**kw):
     f = dict(target=P, draft=None, tokens=P, cu_rows=P, parent=None, slots=None, uniforms=P, accept_len=P, out_tokens=2 * P, out_rows=3 * P, out_slots=None, target_stride=100,
              draft_stride=100, n_seqs=2, n_rows=5, vocab=100)
-    return paged._VerifyArgs(**{**f, **kw})
+    return paged.VerifyArgs(**{**f, **kw})
 
 
 def slots(**kw):
