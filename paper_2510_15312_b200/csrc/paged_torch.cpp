@@ -1,5 +1,5 @@
 // The operators on a cache kept in pages on torch tensors: argument checks, allocation of outputs and the calls of include/sdv.h, for paged.py.  A call
-// takes the host 5.2 us with one output, 7.8 with four or with two launches; through Python checks and ctypes it took 11.2 to 14 (0.4 a tensor checked, 0.7 to 1.4 a tensor
+// takes the host 5.1 us (an append) to 8 (an attention with its workspace and two launches); through Python checks and ctypes it took 11.2 to 14 (0.4 a tensor checked, 0.7 to 1.4 a tensor
 // allocated).  Called on the current device and stream.  What shapes and types do not allow raises
 // ValueError; a status of the library other than SDV_OK is handed back as an int.
 #include <ATen/ATen.h>
@@ -91,11 +91,29 @@ struct Call {
         const Released r;
         return at::detail::empty_cuda(size, type, at::Device(at::kCUDA, (at::DeviceIndex)device), c10::nullopt);
     }
-    at::Tensor fresh(int64_t n, int32_t*& p) const {
-        at::Tensor t = empty({n}, at::kInt);
-        p = t.data_ptr<int32_t>();
+};
+
+// int32 vectors in one allocation, each from a 256-byte boundary on (slots of five trees 6.2 us a call, with four allocations 7.8).
+class Vectors {
+public:
+    Vectors(const Call& c, std::initializer_list<int64_t> lengths) {
+        int64_t total = 0;
+        for (const int64_t n : lengths) total += padded(n);
+        memory_ = c.empty({total}, at::kInt);
+    }
+    at::Tensor next(int64_t n, int32_t*& p) {
+        at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(memory_.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA), memory_.dtype());
+        t.unsafeGetTensorImpl()->set_storage_offset(at_);
+        t.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+        p = n ? memory_.data_ptr<int32_t>() + at_ : nullptr;
+        at_ += padded(n);
         return t;
     }
+
+private:
+    static int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
+    at::Tensor memory_;
+    int64_t at_ = 0;
 };
 
 int type_of(const at::Tensor& t, const char* what) {
@@ -224,10 +242,11 @@ PyObject* slots(PyObject* const* a) {
         s.free_state_out = c.vector(o[3], 2, "free_state (out)");
         slots = tensor(o[0], "slots"), positions = tensor(o[1], "positions"), held = tensor(o[2], "n_held (out)"), state = tensor(o[3], "free_state (out)");
     } else {
-        slots = c.fresh(n_rows, s.slots);
-        positions = c.fresh(n_rows, s.positions);
-        held = c.fresh(n, s.n_held_out);
-        state = c.fresh(2, s.free_state_out);
+        Vectors v(c, {n_rows, n_rows, n, 2});
+        slots = v.next(n_rows, s.slots);
+        positions = v.next(n_rows, s.positions);
+        held = v.next(n, s.n_held_out);
+        state = v.next(2, s.free_state_out);
     }
     return result(released([&] { return g_lib.slots(&s, c.stream); }), {slots, positions, held, state});
 }
@@ -355,10 +374,11 @@ PyObject* verify(PyObject* const* a) {
             moved = tensor(o[3], "slots (out)");
         }
     } else {
-        accept = c.fresh(seqs, s.accept_len);
-        words = c.fresh(n, s.out_tokens);
-        rows = c.fresh(n, s.out_rows);
-        if (s.slots) moved = c.fresh(n, s.out_slots);
+        Vectors v(c, {seqs, n, n, s.slots ? n : 0});
+        accept = v.next(seqs, s.accept_len);
+        words = v.next(n, s.out_tokens);
+        rows = v.next(n, s.out_rows);
+        if (s.slots) moved = v.next(n, s.out_slots);
     }
     return result(n && seqs ? released([&] { return g_lib.verify(&s, c.stream); }) : SDV_OK, {accept, words, rows, moved});
 }
