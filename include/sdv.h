@@ -475,8 +475,8 @@ int sdv_paged_slots(const sdv_slots_args *a, void *cuda_stream);
 /* Rotary embedding with cache append.  Pair i < rot_dim / 2 of a head of q and of k, its elements i and i + rot_dim / 2, or 2i and
  * 2i + 1 when interleaved, is rotated by the angle positions[r] * frequencies[i] (in 64 bits, any int32 position) and scaled by
  * `factor`; elements from rot_dim on pass through.  Computed in 32 bits, rounded once.  q goes to q_out (may be q, with the same strides), k
- * and v go to slot slots[r] of `pages`; a row whose slot is outside the pool (as -1) is not written.  q, or k and v, may be NULL. Of rows that share
- * a slot any one may stay.  rot_dim even, 0 < rot_dim <= head_dim <= 256, head_dim even; any strides, elements of a head contiguous.
+ * and v go to slot slots[r] of `pages`; a row whose slot is outside the pool (as -1) is not written.  q, or k and v, may be NULL.  Rows that share a
+ * slot leave a mixture of them there; k, v and q_out must not lie in the pages, nor k and v at q_out.  rot_dim even, 0 < rot_dim <= head_dim <= 256, head_dim even; any strides, elements of a head contiguous.
  * Accepted rows of a tree reach their consecutive places the same way: the same k, v and positions again, with q NULL and the slots that
  * sdv_verify_sampled gives. */
 typedef struct {
@@ -497,7 +497,7 @@ int sdv_rope_append(const sdv_rope_args *a, const sdv_pages *pages /* NULL witho
  * type for the second product.  What lies in places that a row may not see, infinities and NaN too, does not reach it.  Tokens past
  * table_width * page_size are left out; entries of block_table outside the pool read as zeros.  Rows of a sequence past
  * SDV_TREE_ROWS and rows of no sequence are left as they were in `out`.  `workspace`: sdv_tree_attention_workspace_bytes bytes, 256-byte
- * aligned, contents free before and after; calls that may run at the same time need one each.  status (may be NULL): set to 1 when a wait inside
+ * aligned, contents free before and after; calls that may run at the same time need one each.  out must not be q.  status (may be NULL): set to 1 when a wait inside
  * the kernel ran out, which leaves NaN in the rows concerned; never cleared. */
 typedef struct {
     const void *q;

@@ -61,7 +61,21 @@ int launch(void (*kernel)(KArgs...), int grid, int block, size_t smem, void* str
     at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? SDV_OK : SDV_ECUDA;
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess) return SDV_OK;
+    cudaGetLastError();   // not to be reported by another call's check
+    return SDV_ECUDA;
+}
+
+// No output starts where an input or another output does (those left out are null).
+bool apart(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+    for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
+        if (!*o) continue;
+        for (const void* p : ins)
+            if (p == *o) return false;
+        for (const void* const* other = outs.begin(); other != o; ++other)
+            if (*other == *o) return false;
+    }
+    return true;
 }
 
 // An output's rows (or heads) do not lie on top of each other.
@@ -115,7 +129,9 @@ int prepare_device(int dev) {
         }
         return r;
     });
-    return e == cudaSuccess ? SDV_OK : SDV_ECUDA;
+    if (e == cudaSuccess) return SDV_OK;
+    cudaGetLastError();
+    return SDV_ECUDA;
 }
 
 // Tensor map of 16-bit elements (strides in elements, of every dimension but the first), 128-byte swizzle, zeros outside.
@@ -157,6 +173,8 @@ int sdv_paged_slots(const sdv_slots_args* a, void* cuda_stream) {
     if (!a || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->page_size < 1 || a->table_width < 0 || a->n_free < 0) return SDV_EINVAL;
     if (a->table_stride < a->table_width && a->n_seqs > 1) return SDV_EINVAL;
     if ((long long)a->n_seqs * a->table_width > INT_MAX) return SDV_EINVAL;
+    // blocks read the inputs while others write
+    if (!apart({a->block_table, a->slots, a->positions, a->n_held_out, a->free_state_out}, {a->kv_len, a->cu_rows, a->parent, a->n_held, a->free_pages, a->free_state})) return SDV_EINVAL;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;
     if (!on_device({a->cu_rows, a->free_state, a->free_state_out}, dev, 4)) return SDV_EINVAL;
@@ -164,8 +182,6 @@ int sdv_paged_slots(const sdv_slots_args* a, void* cuda_stream) {
     if (a->n_seqs && a->table_width && !on_device(a->block_table, dev, 4)) return SDV_EINVAL;
     if (a->n_free && !on_device(a->free_pages, dev, 4)) return SDV_EINVAL;
     if (a->n_rows && (!on_device({a->slots, a->positions}, dev, 4) || (a->parent && !on_device(a->parent, dev, 4)))) return SDV_EINVAL;
-    // every block reads what these hold at the start
-    if ((a->n_seqs && a->n_held_out == a->n_held) || a->free_state_out == a->free_state) return SDV_EINVAL;
     const int rc = prepare_device(dev);
     if (rc != SDV_OK) return rc;
     const long long items = (long long)a->n_rows + min((long long)a->n_free, (long long)a->n_seqs * a->table_width);
@@ -178,6 +194,9 @@ int sdv_rope_append(const sdv_rope_args* a, const sdv_pages* pages, void* cuda_s
     if (a->head_dim < 2 || a->head_dim > 256 || a->head_dim % 2 || a->rot_dim < 2 || a->rot_dim > a->head_dim || a->rot_dim % 2) return SDV_EINVAL;
     if ((!a->k) != (!a->v) || (!a->q && !a->k) || (a->q && a->n_q_heads < 1) || (a->k && a->n_kv_heads < 1)) return SDV_EINVAL;
     if (a->q && (!spread(a->n_rows, a->out_row_stride) || !spread(a->n_q_heads, a->out_head_stride))) return SDV_EINVAL;
+    if (a->q && !apart({a->q_out}, {a->k, a->v, a->positions, a->slots, a->frequencies})) return SDV_EINVAL;
+    if (a->q && a->q_out == a->q && ((a->n_rows > 1 && a->out_row_stride != a->q_row_stride) || (a->n_q_heads > 1 && a->out_head_stride != a->q_head_stride))) return SDV_EINVAL;
+    if (a->k && pages && !apart({pages->k, pages->v}, {a->q, a->q ? a->q_out : nullptr, a->k, a->v, a->positions, a->slots, a->frequencies})) return SDV_EINVAL;
     if (a->n_rows == 0) return SDV_OK;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;
@@ -227,6 +246,7 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     if (a->table_stride < a->table_width && a->n_seqs > 1) return SDV_EINVAL;
     if ((a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride) & 7) return SDV_EINVAL;
     if (!spread(a->n_rows, a->out_row_stride) || !spread(a->n_q_heads, a->out_head_stride)) return SDV_EINVAL;
+    if (!apart({a->out, a->workspace, a->status}, {a->q, pages->k, pages->v, a->block_table, a->kv_len, a->cu_rows, a->parent})) return SDV_EINVAL;
     if (a->n_seqs == 0 || a->n_rows == 0 || a->table_width == 0) return SDV_OK;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;
@@ -303,7 +323,7 @@ int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {
     if ((a->draft && a->parent) || (!a->slots) != (!a->out_slots)) return SDV_EINVAL;
     if (a->target_stride < a->vocab || (a->draft && a->draft_stride < a->vocab)) return SDV_EINVAL;
     // a sequence's blocks read what these hold while the first of them writes
-    if (a->out_tokens == a->tokens || a->out_rows == a->tokens || a->out_tokens == a->out_rows || (a->slots && (a->out_slots == a->slots || a->out_slots == a->tokens))) return SDV_EINVAL;
+    if (!apart({a->accept_len, a->out_tokens, a->out_rows, a->out_slots}, {a->target, a->draft, a->tokens, a->cu_rows, a->parent, a->slots, a->uniforms})) return SDV_EINVAL;
     if (a->n_seqs == 0 || a->n_rows == 0) return SDV_OK;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;

@@ -479,3 +479,26 @@ def test_calls_from_several_threads():
     for t in threads:
         t.join()
     assert not wrong
+
+
+def test_a_failed_launch_is_not_reported_by_another_call():
+    """Into a stream whose capture the host has made invalid nothing can be queued; a context that is made afterwards knows nothing of it."""
+    import ctypes as C
+    import torch
+    from paper_2510_15312_b200.binding import Sdv, config_from
+    from sdv_inputs import get_config
+    todo = calls()
+    torch.cuda.synchronize()
+    cudart, s, graph = C.CDLL("libcudart.so.12"), C.c_void_p(), C.c_void_p()
+    assert cudart.cudaStreamCreate(C.byref(s)) == 0 and cudart.cudaStreamBeginCapture(s, 1) == 0
+    assert cudart.cudaStreamSynchronize(s) != 0     # not allowed while capturing
+    cudart.cudaGetLastError()                       # torch's runtime keeps its own, the library has another
+    a = todo[1][1]
+    with pytest.raises(pkg.SdvError):               # (into the pages alone: no output to allocate)
+        pkg.rope_append(*a[:2], k=a[3], v=a[4], k_pages=a[5], v_pages=a[6], slots=a[7], stream=torch.cuda.ExternalStream(s.value))
+    assert cudart.cudaStreamEndCapture(s, C.byref(graph)) != 0 and cudart.cudaStreamDestroy(s) == 0
+    cudart.cudaGetLastError()
+    Sdv(config_from(get_config("tiny"), k_max=8)).close()
+    for name, a, kw in todo:
+        getattr(pkg, name)(*a, **kw)
+    torch.cuda.synchronize()

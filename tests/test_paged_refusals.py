@@ -11,29 +11,29 @@ P = 256   # an address that is never read here
 
 
 def good_pages(**kw):
-    return paged.Pages(**{**dict(k=P, v=P, dtype=0, n_pages=4, page_size=16, n_kv_heads=2, head_dim=64, page_stride=2048, head_stride=1024, token_stride=64), **kw})
+    return paged.Pages(**{**dict(k=8 * P, v=9 * P, dtype=0, n_pages=4, page_size=16, n_kv_heads=2, head_dim=64, page_stride=2048, head_stride=1024, token_stride=64), **kw})
 
 
 def good_slots(**kw):
-    f = dict(kv_len=P, cu_rows=P, parent=None, n_held=P, free_pages=P, free_state=P, block_table=P, slots=P, positions=P, n_held_out=2 * P, free_state_out=2 * P,
+    f = dict(kv_len=P, cu_rows=P, parent=None, n_held=P, free_pages=P, free_state=P, block_table=6 * P, slots=3 * P, positions=4 * P, n_held_out=2 * P, free_state_out=5 * P,
              table_stride=8, n_seqs=2, n_rows=5, page_size=16, table_width=8, n_free=9)
     return paged.SlotsArgs(**{**f, **kw})
 
 
 def good_rope(**kw):
-    f = dict(q=P, k=P, v=P, q_out=P, positions=P, slots=P, frequencies=P, q_row_stride=256, q_head_stride=64, out_row_stride=256, out_head_stride=64, k_row_stride=128,
+    f = dict(q=7 * P, k=P, v=P, q_out=7 * P, positions=P, slots=P, frequencies=P, q_row_stride=256, q_head_stride=64, out_row_stride=256, out_head_stride=64, k_row_stride=128,
              k_head_stride=64, v_row_stride=128, v_head_stride=64, n_rows=5, n_q_heads=4, n_kv_heads=2, head_dim=64, rot_dim=64, interleaved=0, dtype=0, factor=1.0)
     return paged.RopeArgs(**{**f, **kw})
 
 
 def good_attention(**kw):
-    f = dict(q=P, out=P, block_table=P, kv_len=P, cu_rows=P, parent=None, workspace=P, status=None, workspace_bytes=1 << 30, q_row_stride=256, q_head_stride=64,
+    f = dict(q=P, out=2 * P, block_table=P, kv_len=P, cu_rows=P, parent=None, workspace=3 * P, status=None, workspace_bytes=1 << 30, q_row_stride=256, q_head_stride=64,
              out_row_stride=256, out_head_stride=64, table_stride=8, n_seqs=2, n_rows=5, n_q_heads=4, table_width=8, scale=0.125)
     return paged.AttentionArgs(**{**f, **kw})
 
 
 def good_verify(**kw):
-    f = dict(target=P, draft=None, tokens=P, cu_rows=P, parent=None, slots=None, uniforms=P, accept_len=P, out_tokens=2 * P, out_rows=3 * P, out_slots=None, target_stride=100,
+    f = dict(target=P, draft=None, tokens=P, cu_rows=P, parent=None, slots=None, uniforms=P, accept_len=4 * P, out_tokens=2 * P, out_rows=3 * P, out_slots=None, target_stride=100,
              draft_stride=100, n_seqs=2, n_rows=5, vocab=100)
     return paged.VerifyArgs(**{**f, **kw})
 
@@ -55,27 +55,30 @@ def verify(**kw):
 
 
 @pytest.mark.parametrize("kw", [dict(n_seqs=-1), dict(n_seqs=4097), dict(n_rows=-1), dict(page_size=0), dict(table_width=-1), dict(n_free=-1), dict(table_stride=7),
-                                dict(n_seqs=4096, table_width=1 << 20, table_stride=1 << 20)])
+                                dict(n_seqs=4096, table_width=1 << 20, table_stride=1 << 20),
+                                dict(slots=P), dict(slots=4 * P), dict(n_held_out=P), dict(free_state_out=P), dict(block_table=P), dict(positions=6 * P), dict(parent=4 * P)])
 def test_slots_refuses(kw):
     assert slots(**kw) == pkg.EINVAL
 
 
 @pytest.mark.parametrize("kw", [dict(n_rows=-1), dict(dtype=2), dict(head_dim=63), dict(head_dim=258, rot_dim=64), dict(rot_dim=0), dict(rot_dim=66), dict(rot_dim=7), dict(k=None),
-                                dict(v=None), dict(q=None, k=None, v=None), dict(n_q_heads=0), dict(n_kv_heads=0), dict(out_row_stride=0), dict(out_head_stride=-64)])
+                                dict(v=None), dict(q=None, k=None, v=None), dict(n_q_heads=0), dict(n_kv_heads=0), dict(out_row_stride=0), dict(out_head_stride=-64), dict(q_out=P), dict(out_row_stride=512), dict(q_head_stride=128, q_row_stride=512), dict(k=8 * P), dict(v=8 * P),
+                                dict(q_out=9 * P), dict(pages=dict(v=8 * P))])
 def test_rope_refuses(kw):
     assert rope(**kw) == pkg.EINVAL
 
 
 @pytest.mark.parametrize("kw", [dict(n_seqs=-1), dict(n_seqs=4097), dict(n_rows=-1), dict(n_q_heads=3), dict(n_q_heads=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf),
                                 dict(scale=math.nan), dict(table_stride=7), dict(q_row_stride=4), dict(q_head_stride=65), dict(out_row_stride=9), dict(out_head_stride=2),
-                                dict(table_width=-1), dict(out_row_stride=0), dict(out_head_stride=0), dict(n_q_heads=258), dict(pages=dict(head_dim=96)), dict(pages=dict(page_size=24)), dict(pages=dict(page_size=4)), dict(pages=dict(n_kv_heads=0))])
+                                dict(table_width=-1), dict(out_row_stride=0), dict(out_head_stride=0), dict(n_q_heads=258), dict(pages=dict(head_dim=96)), dict(pages=dict(page_size=24)), dict(pages=dict(page_size=4)), dict(pages=dict(n_kv_heads=0)),
+                                dict(out=P), dict(workspace=2 * P), dict(status=P), dict(status=3 * P), dict(out=8 * P), dict(out=9 * P)])
 def test_attention_refuses(kw):
     assert attention(**kw) == pkg.EINVAL
 
 
 @pytest.mark.parametrize("kw", [dict(n_seqs=-1), dict(n_seqs=4097), dict(n_rows=-1), dict(vocab=0), dict(vocab=(1 << 21) + 1, target_stride=1 << 22), dict(target_stride=99),
                                 dict(draft=P, draft_stride=99), dict(draft=P, parent=P), dict(slots=P), dict(out_slots=P), dict(out_tokens=P), dict(out_rows=P), dict(out_rows=2 * P),
-                                dict(slots=5 * P, out_slots=5 * P), dict(slots=5 * P, out_slots=P)])
+                                dict(slots=5 * P, out_slots=5 * P), dict(slots=5 * P, out_slots=P), dict(accept_len=P), dict(accept_len=2 * P), dict(parent=4 * P)])
 def test_verify_refuses(kw):
     assert verify(**kw) == pkg.EINVAL
 
