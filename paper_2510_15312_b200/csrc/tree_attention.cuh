@@ -772,6 +772,8 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
             }
             __syncthreads();
         }
+        // a warp still looks for units to take together while another could be at the next ones
+        if (p0 + gridDim.x * group < tasks) __syncthreads();
     }
 }
 
