@@ -35,10 +35,10 @@ struct SlotShared {
 
 // Pages that sequence b wants; need: those it lacks, 0 where its row of the table is too short for it (fits = false).
 __device__ __forceinline__ long long slots_want(const sdv_slots_args& a, int b, int rows, int& need, bool& narrow) {
-    const long long tokens = (long long)max(__ldg(a.kv_len + b), 0) + rows;
+    const long long tokens = (long long)max(a.kv_len[b], 0) + rows;
     const long long want = rows > 0 ? (tokens + a.page_size - 1) / a.page_size : 0;
     narrow = want > a.table_width;
-    need = narrow ? 0 : max(0, (int)want - min(max(__ldg(a.n_held + b), 0), a.table_width));
+    need = narrow ? 0 : max(0, (int)want - min(max(a.n_held[b], 0), a.table_width));
     return want;
 }
 
@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = a.n_seqs;
     grid_dep_wait();
     grid_dep_launch();   // behind the wait: what comes next may rely on all that came before
-    const int head = max(__ldg(a.free_state), 0);
+    const int head = max(*a.free_state, 0);
     // needs of this thread's sequences, summed up over the block.  The sum of all needs stays below 2^31: each is at most
     // table_width, and the host refuses n_seqs * table_width beyond that.
     const int per = (B + kSlotThreads - 1) / kSlotThreads, b0 = min(tid * per, B), b1 = min(b0 + per, B);
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
             bool narrow;
             slots_want(a, b, max(0, s.row0[b + 1] - s.row0[b]), need, narrow);
             const bool fits = !narrow && taken(b);
-            a.n_held_out[b] = __ldg(a.n_held + b) + (fits ? need : 0);
+            a.n_held_out[b] = a.n_held[b] + (fits ? need : 0);
             if (fits && need) last = head + s.need0[b + 1];
             refused += fits ? 0 : 1;
         }
@@ -106,19 +106,19 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
     const int entries = s.need0[B];
     for (int e = first; e < entries; e += stride) {
         const int b = last_not_above(s.need0, B, e);
-        if (b < B && taken(b)) a.block_table[b * a.table_stride + max(__ldg(a.n_held + b), 0) + (e - s.need0[b])] = __ldg(a.free_pages + head + e);
+        if (b < B && taken(b)) a.block_table[b * a.table_stride + max(a.n_held[b], 0) + (e - s.need0[b])] = a.free_pages[head + e];
     }
     // rows
     for (int r = first; r < a.n_rows; r += stride) {
         const int b = last_not_above(s.row0, B, r);
         int slot = -1, position = 0;
         if (b >= 0 && b < B && r < s.row0[b + 1]) {
-            const int local = r - s.row0[b], length = max(__ldg(a.kv_len + b), 0);
+            const int local = r - s.row0[b], length = max(a.kv_len[b], 0);
             int depth = local;
             if (a.parent) {
                 depth = 0;
                 for (int i = local; i > 0; ++depth) {
-                    const int p = __ldg(a.parent + s.row0[b] + i);
+                    const int p = a.parent[s.row0[b] + i];
                     i = p < 0 || p >= i ? 0 : p;
                 }
             }
@@ -128,9 +128,9 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
             slots_want(a, b, s.row0[b + 1] - s.row0[b], need, narrow);
             if (!narrow && taken(b)) {
                 const long long token = (long long)length + local;
-                const int page_at = (int)(token / a.page_size), offset = (int)(token % a.page_size), held = min(max(__ldg(a.n_held + b), 0), a.table_width);
+                const int page_at = (int)(token / a.page_size), offset = (int)(token % a.page_size), held = min(max(a.n_held[b], 0), a.table_width);
                 // entries behind the held ones may be on their way by another block: from the list, where they come from
-                const int page = page_at < held ? a.block_table[b * a.table_stride + page_at] : __ldg(a.free_pages + head + s.need0[b] + (page_at - held));
+                const int page = page_at < held ? a.block_table[b * a.table_stride + page_at] : a.free_pages[head + s.need0[b] + (page_at - held)];
                 const long long at = (long long)page * a.page_size + offset;
                 slot = page < 0 || at > INT_MAX ? -1 : (int)at;
             }
@@ -179,7 +179,7 @@ __device__ __forceinline__ void rope_turns(const sdv_rope_args& a, int t0, int n
     grid_dep_launch();   // behind the wait: what comes next may rely on all that came before
     for (int i = threadIdx.x; i < n * half; i += kRopeThreads) {
         const int t = i / half, p = i - t * half;
-        const double turns = (double)__ldg(a.positions + t0 + t) * __ldg(a.frequencies + p) * 0.15915494309189533577;   // 1 / (2 pi)
+        const double turns = (double)a.positions[t0 + t] * a.frequencies[p] * 0.15915494309189533577;   // 1 / (2 pi)
         float s, c;
         sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
         turn[i] = make_float2(c * a.factor, s * a.factor);
@@ -196,7 +196,7 @@ __device__ __forceinline__ void rope_turn(T& lo, T& hi, float2 cs) {
 // Where row r of a head goes in the pages; null: nowhere.
 template <typename T>
 __device__ __forceinline__ T* rope_place(const sdv_rope_args& a, const sdv_pages& pages, void* base, int r, int h) {
-    const int slot = __ldg(a.slots + r);
+    const int slot = a.slots[r];
     if (slot < 0 || slot >= (long long)pages.n_pages * pages.page_size) return nullptr;
     const int page = slot / pages.page_size, token = slot - page * pages.page_size;
     return (T*)base + page * pages.page_stride + h * pages.head_stride + token * pages.token_stride;

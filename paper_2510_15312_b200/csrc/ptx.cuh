@@ -323,6 +323,13 @@ __device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.w
 // The next kernel of the stream may start once every block has got here (its own grid_dep_wait still waits for the end).
 __device__ __forceinline__ void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// From L2, whatever L1 holds: before this kernel's own grid_dep_wait, of what was complete before the kernel ahead of it began its work.
+__device__ __forceinline__ int ld_global_l2(const int* p) {
+    int v;
+    asm volatile("ld.global.cg.s32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+
 // 32 bytes in one store (32-byte aligned): a whole L2 sector per thread.
 __device__ __forceinline__ void st_global_v8(void* p, const uint32_t* r) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),

@@ -41,10 +41,11 @@ template <int WARPS>
 struct TreeScan {
     int warp_sum[WARPS], before[WARPS * 32];   // before: within its warp
     __device__ __forceinline__ static int per(const TreeLists& P) { return (P.n_seqs + WARPS * 32 - 1) / (WARPS * 32); }
+    template <bool EARLY>
     __device__ __forceinline__ void fill(const TreeLists& P) {   // all threads; a barrier follows
         const int tid = threadIdx.x, lane = tid & 31, n = per(P), b0 = min(tid * n, P.n_seqs), b1 = min(b0 + n, P.n_seqs);
         int sum = 0;
-        for (int b = b0; b < b1; ++b) sum += tree_tiles(P, tree_seq(P, b));
+        for (int b = b0; b < b1; ++b) sum += tree_tiles(P, tree_seq<EARLY>(P, b));
         int incl = sum;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
@@ -129,11 +130,11 @@ __device__ __forceinline__ void tree_masks(const TreeParams& P, const TreeSeq& s
     m0 = 1ull << lane;
     m1 = 1ull << (lane + 32);
     if (lane > 0 && lane < s.rows) {
-        const int p = __ldg(P.parent + s.first + lane);
+        const int p = P.parent[s.first + lane];
         p0 = p < 0 || p >= lane ? 0 : p;
     }
     if (lane + 32 < s.rows) {
-        const int p = __ldg(P.parent + s.first + lane + 32);
+        const int p = P.parent[s.first + lane + 32];
         p1 = p < 0 || p >= lane + 32 ? 0 : p;
     }
     m0 |= 1ull << p0;
@@ -158,7 +159,7 @@ __device__ __forceinline__ void tree_add_not_finite(const TreeParams& P, const T
 #pragma unroll 1
     for (; rows; rows &= rows - 1) {
         const int key = cur.s.length + __ffsll((long long)rows) - 1;
-        const int page = __ldg(P.block_table + cur.b * P.table_stride + (key >> P.page_shift));
+        const int page = P.block_table[cur.b * P.table_stride + (key >> P.page_shift)];
         if (page < 0 || page >= P.n_pages) continue;
         const T* v = (const T*)P.v + page * P.page_stride + cur.h * P.head_stride + (key & (P.page_size - 1)) * P.token_stride + c;
 #pragma unroll
@@ -223,7 +224,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     if (warp == 5) tmem_alloc(&ctl->tmem_base, 256);   // S0 | S1, 64 columns each | O, HD columns
     if (warp == 4 && lane < 4) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_q1 : lane == 2 ? &map_k : &map_v) : "memory");
     grid_dep_wait();
-    ctl->scan.fill(P);
+    ctl->scan.fill<false>(P);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -251,7 +252,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         bool ok = true;
         const auto page_of = [&](const TreeCursor& c, int tile) {   // page of this lane's box of a tile
             const int key = tile * kTreeKeys + my_box * box_keys;
-            return my_atom < S::kAtoms && key < c.s.keys ? __ldg(P.block_table + c.b * P.table_stride + (key >> P.page_shift)) : -1;
+            return my_atom < S::kAtoms && key < c.s.keys ? P.block_table[c.b * P.table_stride + (key >> P.page_shift)] : -1;
         };
         int page = cur.left > 0 ? page_of(cur, cur.tile) : -1;
         while (cur.left > 0 && ok) {
@@ -612,8 +613,8 @@ __device__ __forceinline__ void tree_gather(const TreeParams& P, const TreeUnit&
         ml[t] = make_float2(-CUDART_INF_F, 0.f);
         if (i < q.n) {
             const int at = q.slot(i, P.blocks) * P.part_rows;
-            ml[t] = __ldcg(ml0 + at);
-            x[t] = __ldcg(reinterpret_cast<const float4*>(o0 + at * HD));
+            ml[t] = ml0[at];
+            x[t] = *reinterpret_cast<const float4*>(o0 + at * HD);
         }
     }
     float mx = m;
@@ -646,13 +647,13 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
     // begins behind ceil(n g / 4) fours, as many broken ones as there are sequences before it, and as many as whole tiles fit n.  (The host sees to it that the number of
     // units stays within 32 bits.)
     const auto first_unit = [&](int b) {
-        const unsigned first = rows_begin(P.cu_rows, b, P.n_rows);
+        const unsigned first = rows_begin<true>(P.cu_rows, b, P.n_rows);
         return (int)((first * P.g + 3u) / 4u + first / P.chunk) + b;
     };
     const int chunk_units = (P.chunk * P.g + 3) / 4;
     const int per = TreeScan<kMergeWarps>::per(P);
     unit0[threadIdx.x] = (int)threadIdx.x * per < P.n_seqs ? first_unit((int)threadIdx.x * per) : INT_MAX;
-    scan.fill(P);
+    scan.fill<true>(P);
     __syncthreads();
     const int total = scan.total(), cols = HD / split;
     const TreeCut cut(total, P.blocks);
@@ -676,8 +677,8 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
                 tile0 += scan.before[t];
                 int b = t * per;
                 const int end = min(b + per, P.n_seqs) - 1;
-                while (b < end && first_unit(b + 1) <= unit) tile0 += tree_tiles(P, tree_seq(P, b++));
-                const TreeSeq s = tree_seq(P, b);
+                while (b < end && first_unit(b + 1) <= unit) tile0 += tree_tiles(P, tree_seq<true>(P, b++));
+                const TreeSeq s = tree_seq<true>(P, b);
                 const int u0 = unit - first_unit(b);
                 if (u0 >= 0 && u0 < s.chunks * chunk_units && s.tiles > 0) {
                     const int c = u0 / chunk_units, rows = min(P.chunk, s.rows - c * P.chunk) * P.g;
@@ -715,12 +716,12 @@ __global__ void __launch_bounds__(kMergeThreads, 3) tree_merge_kernel(const __gr
                     for (int i = 0; i < q.n; i += 2) {   // two parts at a time
                         const int at = q.slot(i, P.blocks) * P.part_rows, next = q.slot(i + 1, P.blocks) * P.part_rows;
                         const bool two = i + 1 < q.n;
-                        const float2 a = __ldcg(row.ml + at), b = two ? __ldcg(row.ml + next) : make_float2(-CUDART_INF_F, 0.f);
+                        const float2 a = row.ml[at], b = two ? row.ml[next] : make_float2(-CUDART_INF_F, 0.f);
                         float4 x[2], y[2];
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
-                            x[g] = __ldcg(reinterpret_cast<const float4*>(row.o + at * HD + (c + g * 32) * 4));
-                            if (two) y[g] = __ldcg(reinterpret_cast<const float4*>(row.o + next * HD + (c + g * 32) * 4));
+                            x[g] = *reinterpret_cast<const float4*>(row.o + at * HD + (c + g * 32) * 4);
+                            if (two) y[g] = *reinterpret_cast<const float4*>(row.o + next * HD + (c + g * 32) * 4);
                         }
                         const float mx = fmaxf(m, fmaxf(a.x, b.x)), ref = mx == -CUDART_INF_F ? 0.f : mx, keep = exp2f(m - ref), fa = exp2f(a.x - ref), fb = exp2f(b.x - ref);
                         m = mx;

@@ -5,16 +5,11 @@
 #include "../../include/sdv.h"
 
 #ifdef __CUDACC__
+#include "ptx.cuh"
 #define SDV_HD __host__ __device__ __forceinline__
 #else
 #define SDV_HD inline
 #endif
-#ifdef __CUDA_ARCH__
-#define SDV_LD(p) __ldg(p)
-#else
-#define SDV_LD(p) (*(p))
-#endif
-
 namespace sdv {
 
 #ifndef __CUDACC__
@@ -33,8 +28,17 @@ struct TreeLists {
     int whole;                                             // items (KV head, row chunk) are dealt out whole, not tile by tile
 };
 
+// An entry of the caller's lists; EARLY: for a kernel that has not waited for the one ahead of it yet (which does not write them, and began behind who did).
+template <bool EARLY>
+SDV_HD int list_entry(const int* p) {
+#ifdef __CUDA_ARCH__
+    if (EARLY) return ld_global_l2(p);
+#endif
+    return *p;
+}
 // Rows of sequence b, whatever cu_rows holds: within [0, n_rows), none where the array descends.
-SDV_HD int rows_begin(const int* cu, int b, int n_rows) { return min(max(SDV_LD(cu + b), 0), n_rows); }
+template <bool EARLY = false>
+SDV_HD int rows_begin(const int* cu, int b, int n_rows) { return min(max(list_entry<EARLY>(cu + b), 0), n_rows); }
 SDV_HD int rows_count(const int* cu, int b, int n_rows) { return max(0, rows_begin(cu, b + 1, n_rows) - rows_begin(cu, b, n_rows)); }
 
 // One sequence as the kernels see it, whatever the arrays hold.
@@ -42,12 +46,13 @@ struct TreeSeq {
     int first, rows, length, keys;     // first row, rows, committed tokens, tokens in all (those the block table has room for)
     int chunks, tiles;                 // tiles of query rows, tiles of keys
 };
+template <bool EARLY = false>
 SDV_HD TreeSeq tree_seq(const TreeLists& P, int b) {
     TreeSeq s;
-    s.first = rows_begin(P.cu_rows, b, P.n_rows);
-    s.rows = min(rows_count(P.cu_rows, b, P.n_rows), SDV_TREE_ROWS);
+    s.first = rows_begin<EARLY>(P.cu_rows, b, P.n_rows);
+    s.rows = min(max(0, rows_begin<EARLY>(P.cu_rows, b + 1, P.n_rows) - s.first), SDV_TREE_ROWS);
     const long long room = min((long long)P.table_width * P.page_size, 0x7fffffffll - kTreeKeys);
-    s.length = (int)min((long long)max(SDV_LD(P.kv_len + b), 0), room);
+    s.length = (int)min((long long)max(list_entry<EARLY>(P.kv_len + b), 0), room);
     s.keys = (int)min((long long)s.length + s.rows, room);
     s.chunks = (s.rows + P.chunk - 1) / P.chunk;
     s.tiles = s.rows ? (s.keys + kTreeKeys - 1) / kTreeKeys : 0;

@@ -89,17 +89,17 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_sampled_kernel(const
         return;
     }
     cluster_arrive_relaxed();   // waited for before anything is written to another block, which has started by then
-    const float draw = __ldg(a.uniforms + first);
+    const float draw = a.uniforms[first];
     const int i = tid;
     float u = 0.f, q = 1.f;
     if (i < SDV_TREE_ROWS) {
         int p = -1, x = -1;
         float s = 0.f;
         if (i > 0 && i < T) {
-            p = a.parent ? __ldg(a.parent + first + i) : i - 1;
+            p = a.parent ? a.parent[first + i] : i - 1;
             if (p < 0 || p >= i) p = 0;
-            x = __ldg(a.tokens + first + i);
-            u = __ldg(a.uniforms + first + i);
+            x = a.tokens[first + i];
+            u = a.uniforms[first + i];
             if (x >= 0 && x < a.vocab) {
                 s = __ldcg(a.target + (first + p) * a.target_stride + x);
                 if (a.draft) q = __ldcg(a.draft + (first + i) * a.draft_stride + x);
@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_sampled_kernel(const
             for (int r = tid; r < all; r += kVerifyThreads) {
                 int to = -1;
                 for (int k = 1; k <= a_len; ++k)
-                    if (path[k] == r && k != r) to = __ldg(a.slots + first + k);
+                    if (path[k] == r && k != r) to = a.slots[first + k];
                 a.out_slots[first + r] = to;
             }
         }
