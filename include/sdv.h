@@ -512,6 +512,9 @@ typedef struct {
 } sdv_attention_args;
 size_t sdv_tree_attention_workspace_bytes(int n_seqs, int head_dim);
 int sdv_tree_attention(const sdv_attention_args *a, const sdv_pages *pages, void *cuda_stream);
+/* Test aid: the same, but every block copies no more than `tiles` tiles of keys and values, as if the others did not arrive, and waits for them run out
+ * after wait_ns (2 s otherwise).  Ends as that does: NaN in the rows concerned, status 1. */
+int sdv_debug_tree_attention(const sdv_attention_args *a, const sdv_pages *pages, unsigned long long wait_ns, int tiles, void *cuda_stream);
 
 /* Verification of drafted tokens against the target's probabilities, with the caller's random numbers u[r] in [0, 1).  target[r] is the target
  * model's distribution behind row r.

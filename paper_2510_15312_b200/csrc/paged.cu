@@ -17,6 +17,7 @@ using namespace sdv;
 
 namespace {
 
+constexpr unsigned long long kWaitNs = 2000000000ull;
 constexpr int kMaxVocab = 1 << 21;   // tile sums of a block of sdv_verify_sampled stay within 32 KB
 
 // Device memory of the current device (where the runtime can tell), on a boundary of `align` bytes.
@@ -238,7 +239,8 @@ size_t sdv_tree_attention_workspace_bytes(int n_seqs, int head_dim) {
     return tree_bytes(head_dim, tree_blocks(dev), kTreeTileRows);
 }
 
-int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void* cuda_stream) {
+// wait_ns: of the waits that may be given up; tiles: see sdv_debug_tree_attention.
+static int tree_attention(const sdv_attention_args* a, const sdv_pages* pages, unsigned long long wait_ns, int tiles, void* cuda_stream) {
     if (!a || !pages || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->table_width < 0) return SDV_EINVAL;
     if (pages->head_dim != 64 && pages->head_dim != 128) return SDV_EINVAL;
     if (pages->page_size < 8 || (pages->page_size & (pages->page_size - 1)) || pages->n_kv_heads < 1) return SDV_EINVAL;
@@ -300,7 +302,9 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     while ((1 << P.page_shift) < pages->page_size) ++P.page_shift;
     P.n_pages = pages->n_pages;
     P.scale_log2e = a->scale * 1.4426950408889634f;
-    P.wait_limit_ns = 2000000000ull;
+    P.copies = 2 * tiles;
+    P.wait_limit_ns = wait_ns;
+    P.drain_limit_ns = kWaitNs;
     CUtensorMap map_q, map_q1, map_k, map_v;
     const int box_keys = min(pages->page_size, kTreeKeys);
     if (!make_page_map(&map_k, pages->k, pages, box_keys) || !make_page_map(&map_v, pages->v, pages, box_keys)) return SDV_EINVAL;
@@ -316,6 +320,12 @@ int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void
     const int split = units * (hd / 16) <= room ? hd / 16 : 1;
     const int group = (int)min((long long)kMergeWarps, (units * split + room - 1) / room);
     return launch(merge_kernel(pages->dtype, hd), (int)min((units * split + group - 1) / group, room), kMergeThreads, 0, cuda_stream, 1, P, group, split);
+}
+
+int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void* cuda_stream) { return tree_attention(a, pages, kWaitNs, INT_MAX / 2, cuda_stream); }
+
+int sdv_debug_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, unsigned long long wait_ns, int tiles, void* cuda_stream) {
+    return tiles < 0 || tiles > INT_MAX / 2 ? SDV_EINVAL : tree_attention(a, pages, wait_ns, tiles, cuda_stream);
 }
 
 int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {

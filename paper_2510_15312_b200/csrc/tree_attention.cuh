@@ -33,7 +33,8 @@ struct TreeParams : TreeLists {
     long long out_row_stride, out_head_stride, table_stride, page_stride, head_stride, token_stride;
     int page_shift, n_pages, part_rows, blocks, q_step;
     float scale_log2e;
-    unsigned long long wait_limit_ns;
+    int copies;                        // keys or values of tiles that a block copies at most: no limit but in tests
+    unsigned long long wait_limit_ns, drain_limit_ns;   // waits that may be given up; those that keep copies and products from outliving the block
 };
 
 // Tiles of all sequences, summed up by a block: thread t has the sequences [t * per, (t + 1) * per).
@@ -260,6 +261,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             TreeCursor nxt = cur;
             nxt.skip(P, n);
             for (int j = 0; j < n && ok; ++j) {
+                if (issued >= P.copies) {
+                    ok = false;
+                    break;
+                }
                 const int tile = cur.tile + j, key = tile * kTreeKeys + my_box * box_keys;
                 const int next_page = j + 1 < n ? page_of(cur, tile + 1) : nxt.left > 0 ? page_of(nxt, nxt.tile) : -1;
                 const bool mine = my_atom < S::kAtoms && key < cur.s.keys;
@@ -286,7 +291,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         for (int back = 0; back < S::kSlots && back < issued; ++back) {
             if (s == 0) { s = S::kSlots; par ^= 1u; }
             --s;
-            if (!mbar_drain(&ctl->full[s], par, P.wait_limit_ns)) break;
+            if (!mbar_drain(&ctl->full[s], par, P.drain_limit_ns)) break;
         }
     } else if (warp == 5) {
         // ---- tensor-core issue
@@ -379,12 +384,12 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             ++item;
             cur = nxt;
         }
-        if (q_loads) mbar_drain(&ctl->q_ready, (q_loads - 1u) & 1u, P.wait_limit_ns);   // where a wait was given up, nobody else waits for the last copy
-        if (!ok) {
-            // behind an abandoned wait: tensor and shared memory are given back only when no product uses them any more
+        if (q_loads) mbar_drain(&ctl->q_ready, (q_loads - 1u) & 1u, P.drain_limit_ns);   // where a wait was given up, nobody else waits for the last copy
+        // tensor and shared memory are given back only when no product uses them any more, whoever gave up a wait: this warp, or those who wait for its last product
+        if (n_s) {
             if (elect_one()) umma_commit(&ctl->drained);
             __syncwarp();
-            mbar_drain(&ctl->drained, 0, P.wait_limit_ns);
+            mbar_drain(&ctl->drained, 0, P.drain_limit_ns);
         }
     } else {
         // ---- softmax: tile row t
