@@ -440,7 +440,7 @@ int sdv_gemm_noalloc(const float *dev_x, const uint16_t *dev_w, float *dev_y, in
  * nothing between calls.  Pointers are checked on the host (alignment; device memory of the current device), sizes too; what
  * lies in device memory is not: the kernels stay within the buffers whatever it holds, as each call says.  Calls
  * that share no output and no workspace may run at the same time.  n_seqs is at most SDV_MAX_SEQUENCES; except for
- * sdv_paged_slots, calls without sequences or rows do nothing.  Errors: SDV_EINVAL, SDV_ENOMEM (workspace), SDV_ECUDA. */
+ * sdv_paged_slots, calls without sequences or rows do nothing, their outputs stay as they were.  Errors: SDV_EINVAL, SDV_ENOMEM (workspace), SDV_ECUDA. */
 #define SDV_MAX_SEQUENCES 4096
 #define SDV_TREE_ROWS 64  /* rows of a sequence that sdv_tree_attention and sdv_verify_sampled take */
 
@@ -525,7 +525,7 @@ int sdv_debug_tree_attention(const sdv_attention_args *a, const sdv_pages *pages
  *   when none is, the next token is drawn from the target's distribution without the rejected tokens.
  * This leaves the target's distribution unchanged.  Drawn: the smallest token whose cumulative sum exceeds u[row 0] * the whole sum, in 64 bits; where nothing is left, from the
  * target's distribution itself, and -1 where that holds nothing either.  Values that are not positive have no share.  Tokens outside the vocabulary are
- * rejected.  Out: accept_len[b] (-1: no rows); out_tokens, from entry cu_rows[b] on, the accept_len[b] accepted tokens and the drawn one; out_rows
+ * rejected.  Out: accept_len[b] (-1: a sequence without rows among others that have some); out_tokens, from entry cu_rows[b] on, the accept_len[b] accepted tokens and the drawn one; out_rows
  * likewise row 0 and the accepted rows, counted from row 0; -1 behind them and for rows of no sequence.  With slots (each row's, from sdv_paged_slots):
  * out_slots[r], where an accepted row's keys and values belong once the others are dropped, -1 for rows that are dropped or lie
  * there already.  Rows past SDV_TREE_ROWS are not looked at.  Probabilities are fp32, vocab at most 2^21, row strides in

@@ -4,6 +4,7 @@
 // ValueError; a status of the library other than SDV_OK is handed back as an int.
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -361,6 +362,7 @@ PyObject* verify(PyObject* const* a) {
     s.tokens = c.vector(a[1], n, "tokens");
     s.cu_rows = c.vector(a[2], seqs + 1, "cu_rows");
     s.parent = c.vector_or_null(a[5], n, "parent");
+    const bool has_slots = given(a[6]);   // (a vector of no rows has no address)
     s.slots = c.vector_or_null(a[6], n, "slots");
     at::Tensor accept, words, rows, moved;
     if (given(a[7])) {
@@ -369,18 +371,24 @@ PyObject* verify(PyObject* const* a) {
         s.out_tokens = c.vector(o[1], n, "tokens (out)");
         s.out_rows = c.vector(o[2], n, "rows (out)");
         accept = tensor(o[0], "accept_len"), words = tensor(o[1], "tokens (out)"), rows = tensor(o[2], "rows (out)");
-        if (s.slots) {
+        if (has_slots) {
             s.out_slots = c.vector(o[3], n, "slots (out)");
             moved = tensor(o[3], "slots (out)");
         }
     } else {
-        Vectors v(c, {seqs, n, n, s.slots ? n : 0});
+        Vectors v(c, {seqs, n, n, has_slots ? n : 0});
         accept = v.next(seqs, s.accept_len);
         words = v.next(n, s.out_tokens);
         rows = v.next(n, s.out_rows);
-        if (s.slots) moved = v.next(n, s.out_slots);
+        if (has_slots) moved = v.next(n, s.out_slots);
     }
-    return result(n && seqs ? released([&] { return g_lib.verify(&s, c.stream); }) : SDV_OK, {accept, words, rows, moved});
+    if (!n || !seqs) {   // the library does nothing: no sequence has rows, no row a sequence
+        const c10::NoGradGuard plain;
+        for (const at::Tensor* t : {&accept, &words, &rows, &moved})
+            if (t->defined() && t->numel()) t->fill_(-1);
+        return result(SDV_OK, {accept, words, rows, moved});
+    }
+    return result(released([&] { return g_lib.verify(&s, c.stream); }), {accept, words, rows, moved});
 }
 
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>

@@ -112,7 +112,8 @@ def tree_attention(q, k_pages, v_pages, block_table, kv_len, cu_rows, parent=Non
 def verify_sampled(target_probs, tokens, cu_rows, uniforms, draft_probs=None, parent=None, slots=None, out=None, stream=None):
     """Accepts drafted tokens against the target's probabilities [rows][vocab] (float32) with the uniform random numbers uniforms [rows] and draws one
     token behind the accepted ones: (accept_len [sequences], tokens [rows], rows [rows], slots [rows] or None).  draft_probs [rows][vocab]: what each draft of a chain was sampled from; without, drafts
-    count as certain (retrieved), and parent may make them trees.  slots: every row's slot, for the slots that accepted rows move to.  out: the tensors to write to."""
+    count as certain (retrieved), and parent may make them trees.  slots: every row's slot, for the slots that accepted rows move to.  A sequence
+    without rows has accept_len -1, also when no sequence has any.  out: the tensors to write to."""
     calls = _calls or _load()
     args = (target_probs, tokens, cu_rows, uniforms, draft_probs, parent, slots, out if out is None else tuple(out))
     r = calls.verify_sampled(*args) if stream is None else _on(stream, "verify_sampled", *args)
