@@ -285,6 +285,7 @@ static int tree_attention(const sdv_attention_args* a, const sdv_pages* pages, u
     P.cu_rows = a->cu_rows;
     P.parent = a->parent;
     P.status = a->status;
+    P.clear = a->clear_rest;
     P.out_row_stride = a->out_row_stride;
     P.out_head_stride = a->out_head_stride;
     P.table_stride = a->table_stride;

@@ -335,7 +335,13 @@ PyObject* attention(PyObject* const* a) {
     s.workspace = workspace.data_ptr();
     s.workspace_bytes = workspace.nbytes();
     s.status = c.vector_or_null(a[10], 1, "status");
-    return result(n && seqs ? released([&] { return g_lib.attention(&s, &p, c.stream); }) : SDV_OK, {out});
+    s.clear_rest = !given(a[8]);   // memory of the allocator's is not handed out as it is
+    if (!n || !seqs || !s.table_width) {   // the library does nothing: no row sees a token
+        const c10::NoGradGuard plain;
+        if (s.clear_rest && n) out.zero_();
+        return result(SDV_OK, {out});
+    }
+    return result(released([&] { return g_lib.attention(&s, &p, c.stream); }), {out});
 }
 
 // (target_probs, tokens, cu_rows, uniforms, draft_probs, parent, slots, out)

@@ -33,6 +33,7 @@ struct TreeParams : TreeLists {
     long long out_row_stride, out_head_stride, table_stride, page_stride, head_stride, token_stride;
     int page_shift, n_pages, part_rows, blocks, q_step;
     float scale_log2e;
+    int clear;                         // rows that nobody computes are filled
     int copies;                        // keys or values of tiles that a block copies at most: no limit but in tests
     unsigned long long wait_limit_ns, drain_limit_ns;   // waits that may be given up; those that keep copies and products from outliving the block
 };
@@ -167,6 +168,27 @@ __device__ __forceinline__ void tree_add_not_finite(const TreeParams& P, const T
         for (int i = 0; i < 32; ++i) {
             const float x = Half16<T>::up(v[i]);
             if (!isfinite(x)) o[i] = __float_as_uint(__uint_as_float(o[i]) + x);
+        }
+    }
+}
+
+// Rows that nobody computes, shared out over the blocks, by one warp: zeros in those of no sequence, NaN in those of a sequence past SDV_TREE_ROWS.
+template <typename T, int HD>
+__device__ __forceinline__ void tree_clear(const TreeParams& P, int lane) {
+    const int words = P.g * P.n_kv * (HD / 8);   // 16 bytes each, of a row
+    const auto fill = [&](int from, int until, uint32_t with) {
+        for (int r = from + (int)blockIdx.x; r < until; r += P.blocks)
+            for (int i = lane; i < words; i += 32)
+                *reinterpret_cast<uint4*>((T*)P.out + r * P.out_row_stride + i / (HD / 8) * P.out_head_stride + i % (HD / 8) * 8) = make_uint4(with, with, with, with);
+    };
+    fill(0, rows_begin(P.cu_rows, 0, P.n_rows), 0u);
+    fill(rows_begin(P.cu_rows, P.n_seqs, P.n_rows), P.n_rows, 0u);
+    for (int b0 = 0; b0 < P.n_seqs; b0 += 32) {
+        const int b = b0 + lane;
+        unsigned many = __ballot_sync(0xffffffffu, b < P.n_seqs && rows_count(P.cu_rows, b, P.n_rows) > SDV_TREE_ROWS);
+        for (; many; many &= many - 1) {
+            const int at = b0 + __ffs(many) - 1;
+            fill(rows_begin(P.cu_rows, at, P.n_rows) + SDV_TREE_ROWS, rows_begin(P.cu_rows, at + 1, P.n_rows), 0x7fff7fffu);
         }
     }
 }
@@ -566,6 +588,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             cur = nxt;
         }
     }
+    if (P.clear && warp == 4) tree_clear<T, HD>(P, lane);   // (the copying warp is the first to be through; from within its branch, the chain over 65536 tokens took 0.5 us more)
     __syncwarp();
     __syncthreads();
     if (warp == 5) tmem_dealloc(tmem, 256);

@@ -101,7 +101,8 @@ def tree_attention_workspace(n_seqs: int, head_dim: int):
 
 def tree_attention(q, k_pages, v_pages, block_table, kv_len, cu_rows, parent=None, scale: Optional[float] = None, out=None, workspace=None, status=None, stream=None):
     """Every row of q [rows][query heads][head dim] attends to the kv_len[b] committed tokens of its sequence and to the rows on its own path through
-    the draft tree, whose keys and values were appended before.  scale: 1 / sqrt(head dim) unless given.  out: like q; rows of no sequence are left as they were.  workspace: see
+    the draft tree, whose keys and values were appended before.  scale: 1 / sqrt(head dim) unless given.  A sequence has at
+    most 64 rows here.  out: like q; rows past the 64th of a sequence and rows of no sequence are left as they were; without one, the first are NaN and the others zeros.  workspace: see
     tree_attention_workspace; without one torch allocates it for the call.  status: int32 [1], set to 1 when a wait inside the kernel ran out."""
     calls = _calls or _load()
     args = (q, k_pages, v_pages, block_table, kv_len, cu_rows, parent, scale, out, workspace, status)

@@ -1,8 +1,10 @@
 """Calls of the operators on pages in which nothing, or not everything, is to be computed: their results say so."""
+import numpy as np
 import pytest
 
 import paper_2510_15312_b200 as pkg
 from test_gpu_paged import i32
+from test_gpu_tree_attention import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +54,71 @@ def test_verify_of_idle_sequences_in_a_graph():
     acc.fill_(3)
     g.replay()
     assert acc.tolist() == [-1, -1]
+
+
+def fresh(c, **kw):
+    """An attention without `out`, in memory that held something else."""
+    import torch
+    dirt = torch.full_like(c.q, 55.0)
+    del dirt
+    return pkg.tree_attention(c.q, c.k, c.v, kw.pop("table", i32(c.table)), i32(c.lengths), i32(c.cu), parent=None if c.parent is None else i32(c.parent), **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("hq,hkv,hd", [(14, 2, 64), (24, 8, 128), (1, 1, 64)])
+@pytest.mark.parametrize("rows,lengths,pad,before", [([3], [5], 6, 0), ([70, 2], [100, 5], 3, 0), ([1, 64, 65, 0, 200], [700, 3, 90, 8, 0], 1, 0), ([2, 90], [10, 10], 400, 7), ([0, 0], [3, 4], 4, 0),
+                                                     ([1] * 100 + [300] + [2] * 50, [9] * 151, 2, 1)])
+def test_attention_without_an_output_to_write_to(rows, lengths, pad, before, hq, hkv, hd, dtype):
+    """Rows of no sequence are zeros, rows past the limit NaN, the others as with a given output."""
+    import torch
+    c = Case(rows, lengths, hq, hkv, hd, 16, dtype, True, seed=2, pad=pad)
+    if before:   # the first rows belong to nobody
+        c.cu = (c.cu + before).astype(np.int32)
+        c.q = torch.cat([c.q[:before], c.q])[:c.n]
+        c.parent = np.concatenate([c.parent[:before], c.parent])[:c.n]
+    want = c.run()
+    kind = np.zeros(c.n, np.int64)
+    for a, b in zip(c.cu[:-1], c.cu[1:]):
+        kind[a:b] = 1
+        kind[a + 64:b] = 2
+    kind = torch.tensor(kind, device="cuda")
+    got = fresh(c)
+    assert torch.equal(got[kind == 1], want[kind == 1])
+    assert bool((got[kind == 0] == 0).all()) and bool(torch.isnan(got[kind == 2]).all())
+    assert bool((want[kind != 1] == 77.0).all())               # a given one: left as they were
+
+
+def test_attention_without_sequences_or_columns():
+    import torch
+    c = Case([2], [20], 4, 2, 64)
+    none = torch.empty((1, 0), dtype=torch.int32, device="cuda")
+    assert bool((fresh(c, table=none) == 0).all())
+    out = torch.full_like(c.q, 77.0)
+    assert bool((fresh(c, table=none, out=out) == 77.0).all())
+    c.lengths, c.cu = [], np.array([0], np.int32)
+    assert bool((fresh(c, table=none[:0]) == 0).all())
+
+
+def test_attention_without_an_output_in_a_graph():
+    """Replayed with other numbers of rows in the same buffers."""
+    import torch
+    c = Case([64, 10], [90, 30], 6, 2, 64, tree=True, pad=0)
+    q, table, kv, cu, parent = c.q, i32(c.table), i32(c.lengths), i32(c.cu), i32(c.parent)
+    call = lambda: pkg.tree_attention(q, c.k, c.v, table, kv, cu, parent=parent)  # noqa: E731
+    call()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = call()
+    for bounds in ([0, 64, 74], [0, 5, 7], [0, 70, 74], [3, 3, 3], [0, 0, 66]):
+        cu.copy_(i32(bounds))
+        got.fill_(55.0)
+        g.replay()
+        given = pkg.tree_attention(q, c.k, c.v, table, kv, cu, parent=parent, out=torch.full_like(q, 77.0))
+        kind = np.zeros(c.n, np.int64)
+        for a, b in zip(bounds[:-1], bounds[1:]):
+            kind[a:b] = 1
+            kind[a + 64:b] = 2
+        kind = torch.tensor(kind, device="cuda")
+        whole = lambda x: torch.nan_to_num(x, nan=-9.0)  # noqa: E731  (a row over tokens that were never appended is anything)
+        assert torch.equal(whole(got[kind == 1]), whole(given[kind == 1]))
+        assert bool((got[kind == 0] == 0).all()) and bool(torch.isnan(got[kind == 2]).all()) and bool((given[kind != 1] == 77.0).all())
