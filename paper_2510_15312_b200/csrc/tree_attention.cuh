@@ -100,6 +100,11 @@ template <typename T> __device__ __forceinline__ uint32_t tree_idesc(uint32_t n)
 template <> __device__ __forceinline__ uint32_t tree_idesc<__nv_bfloat16>(uint32_t n) { return umma_idesc_bf16(128u, n); }
 template <> __device__ __forceinline__ uint32_t tree_idesc<__half>(uint32_t n) { return umma_idesc_bf16(128u, n) & ~((1u << 7) | (1u << 10)); }   // both operands fp16
 
+// Probabilities are relative to 2^shift for a row's largest score.  fp16 has bits for 2^-24 to 2^15.99: with the largest at 2^7 to 2^15, those of 2^-31 of it still count
+// (at 1 to 2^8, a flat tail of 2^-25 each vanished from the outputs but not from the sums: 2^-9 of a row's mass behind 65536 keys).  bf16 has fp32's range.
+template <typename T> constexpr float kProbShift = 0.f;
+template <> constexpr float kProbShift<__half> = 7.f;
+
 // Clears what is infinite or NaN among the two 16-bit numbers of a word; whether there was any.
 template <typename T> __device__ __forceinline__ bool clear_not_finite(uint32_t& w) {
     constexpr uint32_t kExp = Half16<T>::kExponent;
@@ -199,7 +204,7 @@ __device__ __forceinline__ void tree_clear(const TreeParams& P, int lane) {
 // un-normalised outputs, maxima and sums in the workspace.  (Short tables are dealt out in whole items instead, see the host.)
 // Within a block: one warp copies keys and values, box by box of a page, into a ring of tiles (tensor maps: any strides, five tiles of 16 KB in flight a block); one issues S = Q K^T
 // into one of two tensor-memory buffers and, when four warps have turned it into probabilities in place (a tile row a thread, no exchange between threads), P V, which adds up in
-// tensor memory.  The output is rescaled only when a row's maximum grew by more than 2^8: probabilities stay below 2^8 and their sums, in fp32, lose nothing.  S of the next tile is
+// tensor memory.  The output is rescaled only when a row's maximum grew by more than 2^8: probabilities stay below 2^8 (fp16: 2^15, see kProbShift) and their sums, in fp32, lose nothing.  S of the next tile is
 // computed during the softmax of this one.  Probabilities are rounded to the 16-bit type for the second product, as its operand has to be; sums take them unrounded.
 // Bound by memory where the cache is long: 64 sequences of one row over up to 8192 tokens (619 MB, 7 heads a KV head) take 97 us here and 104 with the merge, 5.9 TB/s; a run of
 // many seconds is bound by power, 113 us.  24 trees of up to 40 rows (244 MB) take 49 us: 37 for the bytes, 4 until the first scores, the rest until the slowest block is through
@@ -516,7 +521,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         }
                     }
                     if (grow) m = mx;
-                    const float ref = m == -CUDART_INF_F ? 0.f : m;
+                    const float ref = m == -CUDART_INF_F ? 0.f : m - kProbShift<T>;
                     const uint64_t sc2 = pack_f32x2(P.scale_log2e, P.scale_log2e), ref2 = pack_f32x2(-ref, -ref);
                     uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll
