@@ -437,7 +437,8 @@ int sdv_gemm_noalloc(const float *dev_x, const uint16_t *dev_w, float *dev_y, in
  *
  * All of these calls only queue work on cuda_stream (NULL: the default stream) of the current device and return: they can be
  * captured into a graph, from the second call on each device on (the first one loads code).  They allocate nothing and keep
- * nothing between calls.  Pointers are checked on the host (alignment; device memory of the current device), sizes too; what
+ * nothing between calls.  Pointers are checked on the host (alignment; device memory of the current device; outputs that share memory
+ * with something else are refused), sizes too; what
  * lies in device memory is not: the kernels stay within the buffers whatever it holds, as each call says.  Calls
  * that share no output and no workspace may run at the same time.  n_seqs is at most SDV_MAX_SEQUENCES; except for
  * sdv_paged_slots, calls without sequences or rows do nothing, their outputs stay as they were.  Errors: SDV_EINVAL, SDV_ENOMEM (workspace), SDV_ECUDA. */
@@ -461,7 +462,7 @@ typedef struct {
  * sequence, from entry free_state[0] on, and written behind those it holds.  A sequence whose pages do not fit its row of the
  * table, or that comes when the list has run out, is refused: it gets no page and its rows' slots are -1.  Out: slots and
  * positions of all rows (rows that belong to no sequence: slot -1, position 0), the pages held from now on, and free_state_out =
- * {first unused entry of free_pages, sequences refused}.  Out arrays must not be in arrays.  Entries of block_table and free_pages are
+ * {first unused entry of free_pages, sequences refused}.  Out arrays must not share memory with in arrays or each other.  Entries of block_table and free_pages are
  * not checked against the pool (sdv_rope_append and sdv_tree_attention do that); a negative one gives slot -1. */
 typedef struct {
     const int32_t *kv_len, *cu_rows, *parent, *n_held, *free_pages, *free_state;
@@ -476,7 +477,7 @@ int sdv_paged_slots(const sdv_slots_args *a, void *cuda_stream);
  * 2i + 1 when interleaved, is rotated by the angle positions[r] * frequencies[i] (in 64 bits, any int32 position) and scaled by
  * `factor`; elements from rot_dim on pass through.  Computed in 32 bits, rounded once.  q goes to q_out (may be q, with the same strides), k
  * and v go to slot slots[r] of `pages`; a row whose slot is outside the pool (as -1) is not written.  q, or k and v, may be NULL.  Rows that share a
- * slot leave a mixture of them there; k, v and q_out must not lie in the pages, nor k and v at q_out.  rot_dim even, 0 < rot_dim <= head_dim <= 256, head_dim even; any strides, elements of a head contiguous.
+ * slot leave a mixture of them there; k, v, q and q_out must share no memory with the pages, nor k and v with q_out, nor q with q_out unless they are the same.  rot_dim even, 0 < rot_dim <= head_dim <= 256, head_dim even; any strides, elements of a head contiguous.
  * Accepted rows of a tree reach their consecutive places the same way: the same k, v and positions again, with q NULL and the slots that
  * sdv_verify_sampled gives. */
 typedef struct {
@@ -497,7 +498,7 @@ int sdv_rope_append(const sdv_rope_args *a, const sdv_pages *pages /* NULL witho
  * type for the second product.  What lies in places that a row may not see, infinities and NaN too, does not reach it.  Tokens past
  * table_width * page_size are left out; entries of block_table outside the pool read as zeros.  Rows of a sequence past
  * SDV_TREE_ROWS and rows of no sequence are left as they were in `out` unless clear_rest is set.  With a table of no columns nothing is done.  `workspace`: sdv_tree_attention_workspace_bytes bytes, 256-byte
- * aligned, contents free before and after; calls that may run at the same time need one each.  out must not be q.  status (may be NULL): set to 1 when a wait inside
+ * aligned, contents free before and after; calls that may run at the same time need one each.  out, workspace and status must share no memory with the rest.  status (may be NULL): set to 1 when a wait inside
  * the kernel ran out, which leaves NaN in the rows concerned; never cleared. */
 typedef struct {
     const void *q;
@@ -530,7 +531,7 @@ int sdv_debug_tree_attention(const sdv_attention_args *a, const sdv_pages *pages
  * likewise row 0 and the accepted rows, counted from row 0; -1 behind them and for rows of no sequence.  With slots (each row's, from sdv_paged_slots):
  * out_slots[r], where an accepted row's keys and values belong once the others are dropped, -1 for rows that are dropped or lie
  * there already.  Rows past SDV_TREE_ROWS are not looked at.  Probabilities are fp32, vocab at most 2^21, row strides in
- * elements.  Out arrays must not be in arrays. */
+ * elements.  Out arrays must not share memory with in arrays or each other. */
 typedef struct {
     const float *target, *draft;
     const int32_t *tokens, *cu_rows, *parent, *slots;

@@ -8,7 +8,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsdv.so")
 TORCH_PATH = os.path.join(_HERE, "_paged.so")   # paged.py's calls on torch tensors
 _UNITS = ["sdv.cu", "paged.cu"]   # compiled side by side
-_SOURCES = _UNITS + ["forward.cuh", "dense.cuh", "device_once.h", "layout.cuh", "paged.cuh", "ptx.cuh", "small_gemm.cuh", "small_kernels.cuh",
+_SOURCES = _UNITS + ["forward.cuh", "dense.cuh", "device_once.h", "layout.cuh", "overlap.h", "paged.cuh", "ptx.cuh", "small_gemm.cuh", "small_kernels.cuh",
                      "paged_torch.cpp", "tensor_map.h", "tree_attention.cuh", "tree_plan.h", "verify_sampled.cuh"]
 
 

@@ -8,6 +8,7 @@
 #include <initializer_list>
 
 #include "device_once.h"
+#include "overlap.h"
 #include "paged.cuh"
 #include "tensor_map.h"
 #include "tree_attention.cuh"
@@ -67,7 +68,7 @@ int launch(void (*kernel)(KArgs...), int grid, int block, size_t smem, void* str
     return SDV_ECUDA;
 }
 
-// No output starts where an input or another output does (those left out are null).
+// No output starts where an input or another output does (those left out are null).  Needs no device; how far they reach is looked at once their addresses are known to be real.
 bool apart(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
     for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
         if (!*o) continue;
@@ -77,6 +78,24 @@ bool apart(std::initializer_list<const void*> outs, std::initializer_list<const 
             if (*other == *o) return false;
     }
     return true;
+}
+
+// No output shares memory with an input or another output.
+bool distinct(std::initializer_list<Area> outs, std::initializer_list<Area> ins) {
+    Overlap meet;
+    for (const Area* o = outs.begin(); o != outs.end(); ++o) {
+        for (const Area& a : ins)
+            if (meet(*o, a)) return false;
+        for (const Area* other = outs.begin(); other != o; ++other)
+            if (meet(*o, *other)) return false;
+    }
+    return true;
+}
+Area ints(const void* p, long long n) { return area(p, 4 * n); }
+// [rows][heads][head dim] of 16-bit elements.
+Area heads_area(const void* p, int rows, long long row_stride, int heads, long long head_stride, int dim) { return area(p, 2ll * dim, rows, 2 * row_stride, heads, 2 * head_stride); }
+Area pool_area(const void* p, const sdv_pages& s) {
+    return area(p, 2ll * s.head_dim, s.n_pages, 2 * s.page_stride, s.n_kv_heads, 2 * s.head_stride, s.page_size, 2 * s.token_stride);
 }
 
 // An output's rows (or heads) do not lie on top of each other.
@@ -183,6 +202,10 @@ int sdv_paged_slots(const sdv_slots_args* a, void* cuda_stream) {
     if (a->n_seqs && a->table_width && !on_device(a->block_table, dev, 4)) return SDV_EINVAL;
     if (a->n_free && !on_device(a->free_pages, dev, 4)) return SDV_EINVAL;
     if (a->n_rows && (!on_device({a->slots, a->positions}, dev, 4) || (a->parent && !on_device(a->parent, dev, 4)))) return SDV_EINVAL;
+    if (!distinct({area(a->block_table, 4ll * a->table_width, a->n_seqs, 4 * a->table_stride), ints(a->slots, a->n_rows), ints(a->positions, a->n_rows), ints(a->n_held_out, a->n_seqs),
+                   ints(a->free_state_out, 2)},
+                  {ints(a->kv_len, a->n_seqs), ints(a->cu_rows, a->n_seqs + 1ll), ints(a->parent, a->n_rows), ints(a->n_held, a->n_seqs), ints(a->free_pages, a->n_free), ints(a->free_state, 1)}))
+        return SDV_EINVAL;
     const int rc = prepare_device(dev);
     if (rc != SDV_OK) return rc;
     const long long items = (long long)a->n_rows + min((long long)a->n_free, (long long)a->n_seqs * a->table_width);
@@ -214,6 +237,15 @@ int sdv_rope_append(const sdv_rope_args* a, const sdv_pages* pages, void* cuda_s
         if (!on_device({a->k, a->v}, dev, 2) || !on_device(a->slots, dev, 4) || !pages_ok(pages, dev)) return SDV_EINVAL;
         if (pages->dtype != a->dtype || pages->n_kv_heads != a->n_kv_heads || pages->head_dim != a->head_dim) return SDV_EINVAL;
         bits |= (uintptr_t)a->k >> 1 | (uintptr_t)a->v >> 1 | (uintptr_t)(a->k_row_stride | a->k_head_stride | a->v_row_stride | a->v_head_stride);
+    }
+    {
+        const Area none_there = area(nullptr, 0), positions = ints(a->positions, a->n_rows), frequencies = area(a->frequencies, 4ll * a->rot_dim);
+        const Area q = a->q ? heads_area(a->q, a->n_rows, a->q_row_stride, a->n_q_heads, a->q_head_stride, a->head_dim) : none_there;
+        const Area out = a->q ? heads_area(a->q_out, a->n_rows, a->out_row_stride, a->n_q_heads, a->out_head_stride, a->head_dim) : none_there;
+        const Area k = a->k ? heads_area(a->k, a->n_rows, a->k_row_stride, a->n_kv_heads, a->k_head_stride, a->head_dim) : none_there;
+        const Area v = a->k ? heads_area(a->v, a->n_rows, a->v_row_stride, a->n_kv_heads, a->v_head_stride, a->head_dim) : none_there;
+        const Area slots = a->k ? ints(a->slots, a->n_rows) : none_there, kp = a->k ? pool_area(pages->k, *pages) : none_there, vp = a->k ? pool_area(pages->v, *pages) : none_there;
+        if (!distinct({out, kp, vp}, {k, v, positions, slots, frequencies}) || !distinct({kp, vp}, {q}) || (a->q_out != a->q && !distinct({out}, {q}))) return SDV_EINVAL;
     }
     const int rc = prepare_device(dev);
     if (rc != SDV_OK) return rc;
@@ -274,6 +306,10 @@ static int tree_attention(const sdv_attention_args* a, const sdv_pages* pages, u
     P.blocks = (int)min((long long)tree_blocks(dev), P.whole ? (long long)chunks * pages->n_kv_heads * min(a->n_seqs, a->n_rows) : most);
     P.part_rows = (min(rows, chunk) * g + 3) / 4 * 4;
     if (a->workspace_bytes < tree_bytes(hd, P.blocks, P.part_rows)) return SDV_ENOMEM;
+    if (!distinct({heads_area(a->out, a->n_rows, a->out_row_stride, a->n_q_heads, a->out_head_stride, hd), area(a->workspace, (long long)tree_bytes(hd, P.blocks, P.part_rows)), ints(a->status, 1)},
+                  {heads_area(a->q, a->n_rows, a->q_row_stride, a->n_q_heads, a->q_head_stride, hd), pool_area(pages->k, *pages), pool_area(pages->v, *pages),
+                   area(a->block_table, 4ll * a->table_width, a->n_seqs, 4 * a->table_stride), ints(a->kv_len, a->n_seqs), ints(a->cu_rows, a->n_seqs + 1ll), ints(a->parent, a->n_rows)}))
+        return SDV_EINVAL;
     const size_t parts = (size_t)P.blocks * 2 * P.part_rows;
     uint8_t* ws = (uint8_t*)a->workspace;
     P.part_ml = (float2*)ws;
@@ -340,6 +376,10 @@ int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {
     if (cudaGetDevice(&dev) != cudaSuccess) return SDV_ECUDA;
     if (!on_device({a->target, a->tokens, a->cu_rows, a->uniforms, a->accept_len, a->out_tokens, a->out_rows}, dev, 4)) return SDV_EINVAL;
     if ((a->draft && !on_device(a->draft, dev, 4)) || (a->parent && !on_device(a->parent, dev, 4)) || (a->slots && !on_device({a->slots, a->out_slots}, dev, 4))) return SDV_EINVAL;
+    if (!distinct({ints(a->accept_len, a->n_seqs), ints(a->out_tokens, a->n_rows), ints(a->out_rows, a->n_rows), ints(a->out_slots, a->n_rows)},
+                  {area(a->target, 4ll * a->vocab, a->n_rows, 4 * a->target_stride), area(a->draft, 4ll * a->vocab, a->n_rows, 4 * a->draft_stride), ints(a->tokens, a->n_rows),
+                   ints(a->cu_rows, a->n_seqs + 1ll), ints(a->parent, a->n_rows), ints(a->slots, a->n_rows), ints(a->uniforms, a->n_rows)}))
+        return SDV_EINVAL;
     const int rc = prepare_device(dev);
     if (rc != SDV_OK) return rc;
     // blocks that share a sequence's vocabulary: doubled while every warp keeps a tile and all blocks are resident at once (two an SM)
