@@ -199,8 +199,18 @@ const float* probabilities(const Call& c, PyObject* o, int64_t n, int64_t vocab,
     return t.data_ptr<float>();
 }
 
-PyObject* result(int rc, std::initializer_list<at::Tensor> ts) {
+// The caller's tensors among those that a call wrote to: autograd learns of it, as of torch's own writes in place.
+void wrote(std::initializer_list<PyObject*> os) {
+    for (PyObject* o : os) {
+        if (!given(o)) continue;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();   // (those have no counter)
+    }
+}
+
+PyObject* result(int rc, std::initializer_list<PyObject*> written, std::initializer_list<at::Tensor> ts) {
     if (rc != SDV_OK) return PyLong_FromLong(rc);
+    wrote(written);
     PyObject* out = PyTuple_New((Py_ssize_t)ts.size());
     if (!out) return nullptr;
     Py_ssize_t i = 0;
@@ -235,8 +245,9 @@ PyObject* slots(PyObject* const* a) {
     s.free_state = c.vector(a[5], -1, "free_state");
     s.parent = c.vector_or_null(a[8], n_rows, "parent");
     at::Tensor slots, positions, held, state;
+    PyObject *const none[4] = {Py_None, Py_None, Py_None, Py_None}, *const* o = none;
     if (given(a[9])) {
-        PyObject* const* o = four(a[9], "out: the four tensors slots, positions, n_held and free_state expected");
+        o = four(a[9], "out: the four tensors slots, positions, n_held and free_state expected");
         s.slots = c.vector(o[0], n_rows, "slots");
         s.positions = c.vector(o[1], n_rows, "positions");
         s.n_held_out = c.vector(o[2], n, "n_held (out)");
@@ -249,7 +260,7 @@ PyObject* slots(PyObject* const* a) {
         held = v.next(n, s.n_held_out);
         state = v.next(2, s.free_state_out);
     }
-    return result(released([&] { return g_lib.slots(&s, c.stream); }), {slots, positions, held, state});
+    return result(released([&] { return g_lib.slots(&s, c.stream); }), {a[2], o[0], o[1], o[2], o[3]}, {slots, positions, held, state});
 }
 
 // (positions, frequencies, q, k, v, k_pages, v_pages, slots, interleaved, factor, q_out)
@@ -301,7 +312,8 @@ PyObject* rope(PyObject* const* a) {
         s.q = q.data_ptr();
         s.q_out = out.data_ptr();
     }
-    return result(n ? released([&] { return g_lib.rope(&s, has_k ? &p : nullptr, c.stream); }) : SDV_OK, {out});
+    if (!n) return result(SDV_OK, {}, {out});
+    return result(released([&] { return g_lib.rope(&s, has_k ? &p : nullptr, c.stream); }), {has_k ? a[5] : Py_None, has_k ? a[6] : Py_None, has_q ? a[10] : Py_None}, {out});
 }
 
 // (q, k_pages, v_pages, block_table, kv_len, cu_rows, parent, scale, out, workspace, status)
@@ -339,9 +351,9 @@ PyObject* attention(PyObject* const* a) {
     if (!n || !seqs || !s.table_width) {   // the library does nothing: no row sees a token
         const c10::NoGradGuard plain;
         if (s.clear_rest && n) out.zero_();
-        return result(SDV_OK, {out});
+        return result(SDV_OK, {}, {out});
     }
-    return result(released([&] { return g_lib.attention(&s, &p, c.stream); }), {out});
+    return result(released([&] { return g_lib.attention(&s, &p, c.stream); }), {a[8], a[10]}, {out});
 }
 
 // (target_probs, tokens, cu_rows, uniforms, draft_probs, parent, slots, out)
@@ -371,8 +383,9 @@ PyObject* verify(PyObject* const* a) {
     const bool has_slots = given(a[6]);   // (a vector of no rows has no address)
     s.slots = c.vector_or_null(a[6], n, "slots");
     at::Tensor accept, words, rows, moved;
+    PyObject *const none[4] = {Py_None, Py_None, Py_None, Py_None}, *const* o = none;
     if (given(a[7])) {
-        PyObject* const* o = four(a[7], "out: the four tensors accept_len, tokens, rows and slots (None without slots) expected");
+        o = four(a[7], "out: the four tensors accept_len, tokens, rows and slots (None without slots) expected");
         s.accept_len = c.vector(o[0], seqs, "accept_len");
         s.out_tokens = c.vector(o[1], n, "tokens (out)");
         s.out_rows = c.vector(o[2], n, "rows (out)");
@@ -392,9 +405,9 @@ PyObject* verify(PyObject* const* a) {
         const c10::NoGradGuard plain;
         for (const at::Tensor* t : {&accept, &words, &rows, &moved})
             if (t->defined() && t->numel()) t->fill_(-1);
-        return result(SDV_OK, {accept, words, rows, moved});
+        return result(SDV_OK, {}, {accept, words, rows, moved});
     }
-    return result(released([&] { return g_lib.verify(&s, c.stream); }), {accept, words, rows, moved});
+    return result(released([&] { return g_lib.verify(&s, c.stream); }), {o[0], o[1], o[2], has_slots ? o[3] : Py_None}, {accept, words, rows, moved});
 }
 
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>

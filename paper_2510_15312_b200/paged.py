@@ -2,7 +2,8 @@
 (include/sdv.h says what each computes).  Argument checks, allocation of outputs and the calls are csrc/paged_torch.cpp's; the work is queued on
 the current stream, or on `stream`, and the calls return at once.  All tensors are on the current device; index arrays are int32.  What the tensors' shapes and types
 do not allow raises ValueError, what the library refuses SdvError.  Outputs not passed in are allocated by torch, on the stream the
-work is queued on; the vectors that one call returns share an allocation.  Results carry no gradients."""
+work is queued on; the vectors that one call returns share an allocation.  Results carry no gradients; given tensors that
+a call writes to count as changed in place."""
 from __future__ import annotations
 
 import ctypes as C
