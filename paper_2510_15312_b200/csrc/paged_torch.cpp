@@ -5,6 +5,7 @@
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/GradMode.h>
+#include <c10/core/InferenceMode.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -208,6 +209,14 @@ void wrote(std::initializer_list<PyObject*> os) {
     }
 }
 
+// A whole tensor to one value, as a call would write it: any tensor of the caller's, whatever mode it is from.
+void fill(const at::Tensor& t, int value) {
+    if (!t.defined() || !t.numel()) return;
+    const c10::InferenceMode mode(t.is_inference() || c10::InferenceMode::is_enabled());
+    const c10::NoGradGuard plain;
+    t.fill_(value);
+}
+
 PyObject* result(int rc, std::initializer_list<PyObject*> written, std::initializer_list<at::Tensor> ts) {
     if (rc != SDV_OK) return PyLong_FromLong(rc);
     wrote(written);
@@ -349,8 +358,7 @@ PyObject* attention(PyObject* const* a) {
     s.status = c.vector_or_null(a[10], 1, "status");
     s.clear_rest = !given(a[8]);   // memory of the allocator's is not handed out as it is
     if (!n || !seqs || !s.table_width) {   // the library does nothing: no row sees a token
-        const c10::NoGradGuard plain;
-        if (s.clear_rest && n) out.zero_();
+        if (s.clear_rest) fill(out, 0);
         return result(SDV_OK, {}, {out});
     }
     return result(released([&] { return g_lib.attention(&s, &p, c.stream); }), {a[8], a[10]}, {out});
@@ -402,9 +410,7 @@ PyObject* verify(PyObject* const* a) {
         if (has_slots) moved = v.next(n, s.out_slots);
     }
     if (!n || !seqs) {   // the library does nothing: no sequence has rows, no row a sequence
-        const c10::NoGradGuard plain;
-        for (const at::Tensor* t : {&accept, &words, &rows, &moved})
-            if (t->defined() && t->numel()) t->fill_(-1);
+        for (const at::Tensor* t : {&accept, &words, &rows, &moved}) fill(*t, -1);
         return result(SDV_OK, {}, {accept, words, rows, moved});
     }
     return result(released([&] { return g_lib.verify(&s, c.stream); }), {o[0], o[1], o[2], has_slots ? o[3] : Py_None}, {accept, words, rows, moved});

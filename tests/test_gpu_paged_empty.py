@@ -122,3 +122,16 @@ def test_attention_without_an_output_in_a_graph():
         whole = lambda x: torch.nan_to_num(x, nan=-9.0)  # noqa: E731  (a row over tokens that were never appended is anything)
         assert torch.equal(whole(got[kind == 1]), whole(given[kind == 1]))
         assert bool((got[kind == 0] == 0).all()) and bool(torch.isnan(got[kind == 2]).all()) and bool((given[kind != 1] == 77.0).all())
+
+
+@pytest.mark.parametrize("inside", [False, True])
+def test_idle_calls_in_and_behind_inference_mode(inside):
+    """Outputs made in inference mode are taken outside of it too, as by calls that have something to do, and ordinary ones inside."""
+    import torch
+    with torch.inference_mode(not inside):
+        out = (i32([5, 6]), i32([]), i32([]), None)
+    t, u, cu, e = torch.empty((0, 11), device="cuda"), torch.empty(0, device="cuda"), i32([0, 0, 0]), i32([])
+    with torch.inference_mode(inside):
+        version = None if out[0].is_inference() else out[0]._version
+        acc = pkg.verify_sampled(t, e, cu, u, out=out)[0]
+    assert acc.tolist() == [-1, -1] and (version is None or out[0]._version > version)
