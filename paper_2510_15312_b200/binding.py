@@ -8,7 +8,7 @@ from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
 
-from .build import LIB_PATH, build
+from .build import LIB_PATH, build_library
 
 OK, EINVAL, ENOMEM, ECAPACITY, ESTATE, ECUDA, ETIMEOUT, ETOOBIG = 0, -1, -2, -3, -4, -5, -6, -7
 K_MAX = 31
@@ -60,7 +60,7 @@ def load_library(path: Optional[str] = None):
     global _lib
     if _lib is not None:
         return _lib
-    path = path or build()
+    path = path or build_library()
     L = C.CDLL(path)
     vp, ip, i32p = C.c_void_p, C.POINTER(C.c_int), C.c_void_p
     L.sdv_workspace_bytes.argtypes = [C.POINTER(SdvConfig)]

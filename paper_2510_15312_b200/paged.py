@@ -10,10 +10,9 @@ import ctypes as C
 import math
 from typing import Optional
 
-import torch
-
 from . import binding
 from .binding import EINVAL, SdvError
+from .build import build_torch_calls
 
 _calls = None   # the module of csrc/paged_torch.cpp, once it has the library's entry points
 
@@ -21,10 +20,12 @@ _calls = None   # the module of csrc/paged_torch.cpp, once it has the library's 
 def _load():
     global _calls
     if _calls is None:
+        import torch   # (contexts and the library do without)
         if not torch.cuda.is_available():
             raise SdvError(binding.ECUDA, "no CUDA device (there is no CPU fallback)")
         torch.cuda.init()
-        library = binding.lib()   # builds both if the sources are newer
+        library = binding.lib()
+        build_torch_calls()
         from . import _paged
         _paged.bind(*(C.cast(getattr(library, "sdv_" + n), C.c_void_p).value for n in ("paged_slots", "rope_append", "tree_attention_workspace_bytes", "tree_attention", "verify_sampled")))
         _calls = _paged
@@ -32,6 +33,7 @@ def _load():
 
 
 def _on(stream, name, *args):
+    import torch
     with torch.cuda.stream(stream):
         return getattr(_calls, name)(*args)
 
@@ -93,6 +95,7 @@ def rope_append(positions, frequencies, q=None, k=None, v=None, k_pages=None, v_
 
 def tree_attention_workspace(n_seqs: int, head_dim: int):
     """A workspace for tree_attention on the current device, for up to n_seqs sequences."""
+    import torch
     _load()
     n = binding.lib().sdv_tree_attention_workspace_bytes(n_seqs, head_dim)
     if n == 0:
