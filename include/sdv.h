@@ -440,7 +440,8 @@ int sdv_gemm_noalloc(const float *dev_x, const uint16_t *dev_w, float *dev_y, in
  * nothing between calls.  Pointers are checked on the host (alignment; device memory of the current device; outputs that share memory
  * with something else are refused), sizes too; what
  * lies in device memory is not: the kernels stay within the buffers whatever it holds, as each call says.  Calls
- * that share no output and no workspace may run at the same time.  n_seqs is at most SDV_MAX_SEQUENCES; except for
+ * that share no output and no workspace may run at the same time.  n_seqs is at most SDV_MAX_SEQUENCES, n_rows and the elements of a
+ * row at most 2^30; except for
  * sdv_paged_slots, calls without sequences or rows do nothing, their outputs stay as they were.  Errors: SDV_EINVAL, SDV_ENOMEM (workspace), SDV_ECUDA. */
 #define SDV_MAX_SEQUENCES 4096
 #define SDV_TREE_ROWS 64  /* rows of a sequence that sdv_tree_attention and sdv_verify_sampled take */

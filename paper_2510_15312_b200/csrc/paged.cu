@@ -19,6 +19,7 @@ using namespace sdv;
 namespace {
 
 constexpr unsigned long long kWaitNs = 2000000000ull;
+constexpr int kMaxRows = 1 << 30;    // row numbers plus a grid's stride stay within 32 bits, and the elements of a row of heads
 constexpr int kMaxVocab = 1 << 21;   // tile sums of a block of sdv_verify_sampled stay within 32 KB
 
 // Device memory of the current device (where the runtime can tell), on a boundary of `align` bytes.
@@ -190,7 +191,7 @@ size_t tree_bytes(int head_dim, int blocks, int rows) {
 extern "C" {
 
 int sdv_paged_slots(const sdv_slots_args* a, void* cuda_stream) {
-    if (!a || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->page_size < 1 || a->table_width < 0 || a->n_free < 0) return SDV_EINVAL;
+    if (!a || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->n_rows > kMaxRows || a->page_size < 1 || a->table_width < 0 || a->n_free < 0) return SDV_EINVAL;
     if (a->table_stride < a->table_width && a->n_seqs > 1) return SDV_EINVAL;
     if ((long long)a->n_seqs * a->table_width > INT_MAX) return SDV_EINVAL;
     // blocks read the inputs while others write
@@ -214,9 +215,10 @@ int sdv_paged_slots(const sdv_slots_args* a, void* cuda_stream) {
 }
 
 int sdv_rope_append(const sdv_rope_args* a, const sdv_pages* pages, void* cuda_stream) {
-    if (!a || a->n_rows < 0 || (a->dtype != SDV_BF16 && a->dtype != SDV_FP16)) return SDV_EINVAL;
+    if (!a || a->n_rows < 0 || a->n_rows > kMaxRows || (a->dtype != SDV_BF16 && a->dtype != SDV_FP16)) return SDV_EINVAL;
     if (a->head_dim < 2 || a->head_dim > 256 || a->head_dim % 2 || a->rot_dim < 2 || a->rot_dim > a->head_dim || a->rot_dim % 2) return SDV_EINVAL;
     if ((!a->k) != (!a->v) || (!a->q && !a->k) || (a->q && a->n_q_heads < 1) || (a->k && a->n_kv_heads < 1)) return SDV_EINVAL;
+    if (((a->q ? (long long)a->n_q_heads : 0) + (a->k ? 2ll * a->n_kv_heads : 0)) * a->head_dim > kMaxRows) return SDV_EINVAL;
     if (a->q && (!spread(a->n_rows, a->out_row_stride) || !spread(a->n_q_heads, a->out_head_stride))) return SDV_EINVAL;
     if (a->q && !apart({a->q_out}, {a->k, a->v, a->positions, a->slots, a->frequencies})) return SDV_EINVAL;
     if (a->q && a->q_out == a->q && ((a->n_rows > 1 && a->out_row_stride != a->q_row_stride) || (a->n_q_heads > 1 && a->out_head_stride != a->q_head_stride))) return SDV_EINVAL;
@@ -366,7 +368,7 @@ int sdv_debug_tree_attention(const sdv_attention_args* a, const sdv_pages* pages
 }
 
 int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {
-    if (!a || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->vocab < 1 || a->vocab > kMaxVocab) return SDV_EINVAL;
+    if (!a || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->n_rows > kMaxRows || a->vocab < 1 || a->vocab > kMaxVocab) return SDV_EINVAL;
     if ((a->draft && a->parent) || (!a->slots) != (!a->out_slots)) return SDV_EINVAL;
     if (a->target_stride < a->vocab || (a->draft && a->draft_stride < a->vocab)) return SDV_EINVAL;
     // a sequence's blocks read what these hold while the first of them writes
