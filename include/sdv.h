@@ -464,7 +464,8 @@ typedef struct {
  * table, or that comes when the list has run out, is refused: it gets no page and its rows' slots are -1.  Out: slots and
  * positions of all rows (rows that belong to no sequence: slot -1, position 0), the pages held from now on, and free_state_out =
  * {first unused entry of free_pages, sequences refused}.  Out arrays must not share memory with in arrays or each other.  Entries of block_table and free_pages are
- * not checked against the pool (sdv_rope_append and sdv_tree_attention do that); a negative one gives slot -1. */
+ * not checked against the pool (sdv_rope_append and sdv_tree_attention do that); a negative one gives slot -1.
+ * With parent n_rows is at most SDV_MAX_SEQUENCES * SDV_TREE_ROWS: every row's depth is walked, 50 ns a step. */
 typedef struct {
     const int32_t *kv_len, *cu_rows, *parent, *n_held, *free_pages, *free_state;
     int32_t *block_table;   /* [n_seqs][table_width], rows table_stride apart; updated */

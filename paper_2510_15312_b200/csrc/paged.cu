@@ -193,6 +193,7 @@ extern "C" {
 int sdv_paged_slots(const sdv_slots_args* a, void* cuda_stream) {
     if (!a || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->n_rows > kMaxRows || a->page_size < 1 || a->table_width < 0 || a->n_free < 0) return SDV_EINVAL;
     if (a->table_stride < a->table_width && a->n_seqs > 1) return SDV_EINVAL;
+    if (a->parent && a->n_rows > SDV_MAX_SEQUENCES * SDV_TREE_ROWS) return SDV_EINVAL;
     if ((long long)a->n_seqs * a->table_width > INT_MAX) return SDV_EINVAL;
     // blocks read the inputs while others write
     if (!apart({a->block_table, a->slots, a->positions, a->n_held_out, a->free_state_out}, {a->kv_len, a->cu_rows, a->parent, a->n_held, a->free_pages, a->free_state})) return SDV_EINVAL;

@@ -45,7 +45,7 @@ def _fail(rc: int, where: str):
 def paged_slots(kv_len, cu_rows, block_table, n_held, free_pages, free_state, page_size: int, n_rows: int, parent=None, out=None, stream=None):
     """Hands pages to the sequences that need more and gives every row its slot and position: (slots, positions, n_held, free_state) after the call;
     block_table [sequences][width] is updated in place.  free_state[0] is the first unused entry of free_pages; of the returned one, the second entry is the number of
-    sequences that were refused for want of pages (their slots are -1).  out: the four tensors to write to."""
+    sequences that were refused for want of pages (their slots are -1).  With parent, at most 262144 rows.  out: the four tensors to write to."""
     calls = _calls or _load()
     args = (kv_len, cu_rows, block_table, n_held, free_pages, free_state, page_size, n_rows, parent, out if out is None else tuple(out))
     r = calls.paged_slots(*args) if stream is None else _on(stream, "paged_slots", *args)

@@ -25,3 +25,9 @@ def test_elements_of_a_row(kw):
 
 def test_the_longest_rows():
     assert taken(rope(n_q_heads=(MOST >> 6) - 4, out_row_stride=2 ** 34, q_row_stride=2 ** 34))
+
+
+def test_rows_with_parents():
+    """A row's depth is walked step by step: a chain of n rows takes n^2 / 2 of them in all, so n is bounded."""
+    assert slots(parent=7 * 256, n_rows=4096 * 64 + 1) == pkg.EINVAL
+    assert taken(slots(parent=7 * 256, n_rows=4096 * 64)) and taken(slots(n_rows=4096 * 64 + 1))
