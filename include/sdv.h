@@ -499,7 +499,7 @@ int sdv_rope_append(const sdv_rope_args *a, const sdv_pages *pages /* NULL witho
  * at most 2^30 tiles of 64 keys.  Scores, statistics and sums in fp32, probabilities rounded to the 16-bit
  * type for the second product.  What lies in places that a row may not see, infinities and NaN too, does not reach it.  Tokens past
  * table_width * page_size are left out; entries of block_table outside the pool read as zeros.  Rows of a sequence past
- * SDV_TREE_ROWS and rows of no sequence are left as they were in `out` unless clear_rest is set.  With a table of no columns nothing is done.  `workspace`: sdv_tree_attention_workspace_bytes bytes, 256-byte
+ * SDV_TREE_ROWS and rows of no sequence are left as they were in `out`.  With a table of no columns nothing is done.  `workspace`: sdv_tree_attention_workspace_bytes bytes, 256-byte
  * aligned, contents free before and after; calls that may run at the same time need one each.  out, workspace and status must share no memory with the rest.  status (may be NULL): set to 1 when a wait inside
  * the kernel ran out, which leaves NaN in the rows concerned; never cleared. */
 typedef struct {
@@ -512,10 +512,11 @@ typedef struct {
     long long q_row_stride, q_head_stride, out_row_stride, out_head_stride, table_stride;
     int n_seqs, n_rows, n_q_heads, table_width;
     float scale;
-    int clear_rest;   /* non-zero: rows of no sequence become zeros in `out`, rows of a sequence past SDV_TREE_ROWS NaN */
 } sdv_attention_args;
 size_t sdv_tree_attention_workspace_bytes(int n_seqs, int head_dim);
 int sdv_tree_attention(const sdv_attention_args *a, const sdv_pages *pages, void *cuda_stream);
+/* The same for an `out` that nothing was written to before: rows of no sequence become zeros, rows of a sequence past SDV_TREE_ROWS NaN. */
+int sdv_tree_attention_fresh(const sdv_attention_args *a, const sdv_pages *pages, void *cuda_stream);
 /* Test aid: the same, but every block copies no more than `tiles` tiles of keys and values, as if the others did not arrive, and waits for them run out
  * after wait_ns (2 s otherwise).  Ends as that does: NaN in the rows concerned, status 1. */
 int sdv_debug_tree_attention(const sdv_attention_args *a, const sdv_pages *pages, unsigned long long wait_ns, int tiles, void *cuda_stream);

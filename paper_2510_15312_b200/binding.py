@@ -24,7 +24,7 @@ EXPORTS = [
     "sdv_debug_top_successors",
     "sdv_follower_workspace_bytes", "sdv_create_follower", "sdv_verify_batch", "sdv_get_verified",
     "sdv_decode_steps", "sdv_run_kernel_ms", "sdv_step",
-    "sdv_paged_slots", "sdv_rope_append", "sdv_tree_attention_workspace_bytes", "sdv_tree_attention", "sdv_debug_tree_attention", "sdv_verify_sampled",
+    "sdv_paged_slots", "sdv_rope_append", "sdv_tree_attention_workspace_bytes", "sdv_tree_attention", "sdv_tree_attention_fresh", "sdv_debug_tree_attention", "sdv_verify_sampled",
 ]
 
 
@@ -120,6 +120,7 @@ def load_library(path: Optional[str] = None):
     L.sdv_tree_attention_workspace_bytes.argtypes = [C.c_int, C.c_int]
     L.sdv_tree_attention_workspace_bytes.restype = C.c_size_t
     L.sdv_tree_attention.argtypes = [vp, vp, vp]
+    L.sdv_tree_attention_fresh.argtypes = [vp, vp, vp]
     L.sdv_debug_tree_attention.argtypes = [vp, vp, C.c_ulonglong, C.c_int, vp]
     L.sdv_verify_sampled.argtypes = [vp, vp]
     for name in EXPORTS:

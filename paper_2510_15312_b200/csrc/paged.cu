@@ -274,8 +274,8 @@ size_t sdv_tree_attention_workspace_bytes(int n_seqs, int head_dim) {
     return tree_bytes(head_dim, tree_blocks(dev), kTreeTileRows);
 }
 
-// wait_ns: of the waits that may be given up; tiles: see sdv_debug_tree_attention.
-static int tree_attention(const sdv_attention_args* a, const sdv_pages* pages, unsigned long long wait_ns, int tiles, void* cuda_stream) {
+// clear: see sdv_tree_attention_fresh; wait_ns: of the waits that may be given up; tiles: see sdv_debug_tree_attention.
+static int tree_attention(const sdv_attention_args* a, const sdv_pages* pages, bool clear, unsigned long long wait_ns, int tiles, void* cuda_stream) {
     if (!a || !pages || a->n_seqs < 0 || a->n_seqs > SDV_MAX_SEQUENCES || a->n_rows < 0 || a->table_width < 0) return SDV_EINVAL;
     if (pages->head_dim != 64 && pages->head_dim != 128) return SDV_EINVAL;
     if (pages->page_size < 8 || (pages->page_size & (pages->page_size - 1)) || pages->n_kv_heads < 1) return SDV_EINVAL;
@@ -324,7 +324,7 @@ static int tree_attention(const sdv_attention_args* a, const sdv_pages* pages, u
     P.cu_rows = a->cu_rows;
     P.parent = a->parent;
     P.status = a->status;
-    P.clear = a->clear_rest;
+    P.clear = clear;
     P.out_row_stride = a->out_row_stride;
     P.out_head_stride = a->out_head_stride;
     P.table_stride = a->table_stride;
@@ -362,10 +362,12 @@ static int tree_attention(const sdv_attention_args* a, const sdv_pages* pages, u
     return launch(merge_kernel(pages->dtype, hd), (int)min((units * split + group - 1) / group, room), kMergeThreads, 0, cuda_stream, 1, P, group, split);
 }
 
-int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void* cuda_stream) { return tree_attention(a, pages, kWaitNs, INT_MAX / 2, cuda_stream); }
+int sdv_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, void* cuda_stream) { return tree_attention(a, pages, false, kWaitNs, INT_MAX / 2, cuda_stream); }
+
+int sdv_tree_attention_fresh(const sdv_attention_args* a, const sdv_pages* pages, void* cuda_stream) { return tree_attention(a, pages, true, kWaitNs, INT_MAX / 2, cuda_stream); }
 
 int sdv_debug_tree_attention(const sdv_attention_args* a, const sdv_pages* pages, unsigned long long wait_ns, int tiles, void* cuda_stream) {
-    return tiles < 0 || tiles > INT_MAX / 2 ? SDV_EINVAL : tree_attention(a, pages, wait_ns, tiles, cuda_stream);
+    return tiles < 0 || tiles > INT_MAX / 2 ? SDV_EINVAL : tree_attention(a, pages, false, wait_ns, tiles, cuda_stream);
 }
 
 int sdv_verify_sampled(const sdv_verify_args* a, void* cuda_stream) {

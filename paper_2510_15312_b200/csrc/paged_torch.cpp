@@ -23,7 +23,7 @@ struct Library {
     decltype(&sdv_paged_slots) slots;
     decltype(&sdv_rope_append) rope;
     decltype(&sdv_tree_attention_workspace_bytes) workspace_bytes;
-    decltype(&sdv_tree_attention) attention;
+    decltype(&sdv_tree_attention) attention, attention_fresh;
     decltype(&sdv_verify_sampled) verify;
 };
 Library g_lib{};
@@ -356,12 +356,12 @@ PyObject* attention(PyObject* const* a) {
     s.workspace = workspace.data_ptr();
     s.workspace_bytes = workspace.nbytes();
     s.status = c.vector_or_null(a[10], 1, "status");
-    s.clear_rest = !given(a[8]);   // memory of the allocator's is not handed out as it is
+    const bool fresh = !given(a[8]);   // memory of the allocator's is not handed out as it is
     if (!n || !seqs || !s.table_width) {   // the library does nothing: no row sees a token
-        if (s.clear_rest) fill(out, 0);
+        if (fresh) fill(out, 0);
         return result(SDV_OK, {}, {out});
     }
-    return result(released([&] { return g_lib.attention(&s, &p, c.stream); }), {a[8], a[10]}, {out});
+    return result(released([&] { return (fresh ? g_lib.attention_fresh : g_lib.attention)(&s, &p, c.stream); }), {a[8], a[10]}, {out});
 }
 
 // (target_probs, tokens, cu_rows, uniforms, draft_probs, parent, slots, out)
@@ -431,14 +431,14 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// The addresses of the library's five entry points, in the order of Library.
+// The addresses of the library's six entry points, in the order of Library.
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    void* p[5];
-    if (n != 5) {
-        PyErr_SetString(PyExc_TypeError, "five addresses expected");
+    void* p[6];
+    if (n != 6) {
+        PyErr_SetString(PyExc_TypeError, "six addresses expected");
         return nullptr;
     }
-    for (int i = 0; i < 5; ++i) {
+    for (int i = 0; i < 6; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (!p[i] && PyErr_Occurred()) return nullptr;
     }
@@ -446,7 +446,8 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     g_lib.rope = (decltype(g_lib.rope))p[1];
     g_lib.workspace_bytes = (decltype(g_lib.workspace_bytes))p[2];
     g_lib.attention = (decltype(g_lib.attention))p[3];
-    g_lib.verify = (decltype(g_lib.verify))p[4];
+    g_lib.attention_fresh = (decltype(g_lib.attention_fresh))p[4];
+    g_lib.verify = (decltype(g_lib.verify))p[5];
     Py_RETURN_NONE;
 }
 

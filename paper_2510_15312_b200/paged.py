@@ -27,7 +27,7 @@ def _load():
         library = binding.lib()
         build_torch_calls()
         from . import _paged
-        _paged.bind(*(C.cast(getattr(library, "sdv_" + n), C.c_void_p).value for n in ("paged_slots", "rope_append", "tree_attention_workspace_bytes", "tree_attention", "verify_sampled")))
+        _paged.bind(*(C.cast(getattr(library, "sdv_" + n), C.c_void_p).value for n in ("paged_slots", "rope_append", "tree_attention_workspace_bytes", "tree_attention", "tree_attention_fresh", "verify_sampled")))
         _calls = _paged
     return _calls
 

@@ -135,3 +135,24 @@ def test_idle_calls_in_and_behind_inference_mode(inside):
         version = None if out[0].is_inference() else out[0]._version
         acc = pkg.verify_sampled(t, e, cu, u, out=out)[0]
     assert acc.tolist() == [-1, -1] and (version is None or out[0]._version > version)
+
+
+def test_the_bytes_behind_the_last_field_of_the_arguments_say_nothing():
+    """The C call leaves rows that nobody computes as they were, whatever lies in the padding of its structure."""
+    import ctypes as C
+    import torch
+    from paged_structs import AttentionArgs, Pages
+    c = Case([2], [20], 4, 2, 64)
+    out, ws = torch.full_like(c.q, 77.0), pkg.tree_attention_workspace(1, 64)
+    table, lengths, cu = i32(c.table), i32(c.lengths), i32(c.cu)
+    pages = Pages(c.k.data_ptr(), c.v.data_ptr(), 0, c.k.shape[0], 16, 2, 64, *c.k.stride()[:3])
+    args = AttentionArgs(q=c.q.data_ptr(), out=out.data_ptr(), block_table=table.data_ptr(), kv_len=lengths.data_ptr(), cu_rows=cu.data_ptr(), workspace=ws.data_ptr(),
+                         workspace_bytes=ws.numel(), q_row_stride=256, q_head_stride=64, out_row_stride=256, out_head_stride=64, table_stride=table.stride(0), n_seqs=1, n_rows=c.n,
+                         n_q_heads=4, table_width=table.shape[1], scale=0.125)
+    end = AttentionArgs.scale.offset + 4
+    C.memset(C.addressof(args) + end, 0xff, C.sizeof(args) - end)
+    stream = C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    for call, rest in ((pkg.lib().sdv_tree_attention, 77.0), (pkg.lib().sdv_tree_attention_fresh, 0.0)):
+        assert call(C.byref(args), C.byref(pages), stream) == pkg.OK
+        torch.cuda.synchronize()
+        assert bool((out[2:] == rest).all()) and torch.equal(out[:2], c.run()[:2])
