@@ -529,7 +529,7 @@ int sdv_debug_tree_attention(const sdv_attention_args *a, const sdv_pages *pages
  *   is accepted when u[r] * (1 - the target's shares of the tokens rejected before it) < target[x], a token rejected before having no share;
  *   when none is, the next token is drawn from the target's distribution without the rejected tokens.
  * This leaves the target's distribution unchanged.  Drawn: the smallest token whose cumulative sum exceeds u[row 0] * the whole sum, in 64 bits; where nothing is left, from the
- * target's distribution itself, and -1 where that holds nothing either.  Values that are not positive have no share.  Tokens outside the vocabulary are
+ * target's distribution itself, and -1 where that holds nothing either.  Values of target that are not positive have no share, draft's negative ones count as 0.  Tokens outside the vocabulary are
  * rejected.  Out: accept_len[b] (-1: a sequence without rows among others that have some); out_tokens, from entry cu_rows[b] on, the accept_len[b] accepted tokens and the drawn one; out_rows
  * likewise row 0 and the accepted rows, counted from row 0; -1 behind them and for rows of no sequence.  With slots (each row's, from sdv_paged_slots):
  * out_slots[r], where an accepted row's keys and values belong once the others are dropped, -1 for rows that are dropped or lie

@@ -55,7 +55,7 @@ __device__ __forceinline__ void verify_load(const VerifyRest& d, int first, int 
         if (!d.q) q[i] = 0.f;
         const bool has = p[i] > 0.f && p[i] > q[i];   // NaN has none
         p[i] = has ? p[i] : 0.f;
-        q[i] = has ? q[i] : 0.f;
+        q[i] = has ? fmaxf(q[i], 0.f) : 0.f;
     }
 }
 
@@ -102,7 +102,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_sampled_kernel(const
             u = a.uniforms[first + i];
             if (x >= 0 && x < a.vocab) {
                 s = __ldcg(a.target + (first + p) * a.target_stride + x);
-                if (a.draft) q = __ldcg(a.draft + (first + i) * a.draft_stride + x);
+                if (a.draft) {
+                    q = __ldcg(a.draft + (first + i) * a.draft_stride + x);
+                    if (q < 0.f) q = 0.f;
+                }
             }
         }
         tok[i] = x;
