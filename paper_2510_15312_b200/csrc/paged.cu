@@ -302,8 +302,12 @@ static int tree_attention(const sdv_attention_args* a, const sdv_pages* pages, b
     const long long each = ((keys + kTreeKeys - 1) / kTreeKeys) * chunks * pages->n_kv_heads, most = each * min(a->n_seqs, a->n_rows);   // no more tiles than this
     if (each * a->n_seqs > INT_MAX / 2) return SDV_EINVAL;   // (whatever cu_rows holds)
     // Short tables: a block goes through whole items and nothing is merged, which saves a launch (2 us on the host) and the merge (2 to 5 us).  Tile by tile against whole,
-    // device time in us: one sequence, four tiles of 64 keys 8.8 : 9.3 (two 8.8 : 7.2, eight 8.9 : 13.3), 64 sequences of one row with 12 + 2 heads, eight tiles 16.2 :
-    // 15.4 (twelve 19.0 : 20.6), of 20 rows with 24 + 8 heads 45 : 32.
+    // device time in us, by sequences x rows:
+    //   4 + 4 heads of 64     1 x 1: 2 tiles of 64 keys 8.2:6.5, 4 8.3:8.0, 6 8.3:9.5     64 x 20: 4 13.8:9.3, 8 16.7:12.9, 10 18.2:14.7, 16 23.0:20.2     300 x 1: 6 37.4:36.6, 8 43.7:44.7
+    //   12 + 2 heads of 128   1 x 1: 2 9.0:7.5, 4 9.0:9.3, 6 9.1:11.3                     64 x 1: 8 16.7:15.4, 10 17.3:17.7     64 x 20: 8 25.6:17.5, 10 26.9:20.0, 16 32.2:27.4
+    //   24 + 8 heads of 128   1 x 17: 4 10.6:9.5, 6 11.8:11.6, 8 12.9:13.4                64 x 20: 8 45.7:32.3, 10 51.9:37.6, 16 66.6:52.9     300 x 1: 8 111.9:110.2, 12 158.5:159.5
+    // The rule knows the table's width, not the rows, heads and lengths: it takes shares where many sequences have many rows behind tables of more than eight tiles, up to 38 percent slower,
+    // and whole items for hundreds of single rows, up to 3 percent slower.
     const long long key_tiles = (keys + kTreeKeys - 1) / kTreeKeys;
     P.whole = key_tiles <= 4 || (key_tiles <= 8 && a->n_seqs >= 8);
     P.blocks = (int)min((long long)tree_blocks(dev), P.whole ? (long long)chunks * pages->n_kv_heads * min(a->n_seqs, a->n_rows) : most);

@@ -206,7 +206,7 @@ __device__ __forceinline__ T* rope_place(const sdv_rope_args& a, const sdv_pages
 
 // A block takes `tokens` rows: their cosines and sines once, then all heads of q, k and v in units of 2 W elements, W on either side of the pairs (half layout: only where
 // the halves are multiples of W) or W neighbouring pairs.  A unit is read whole before it is written, so q may be turned in place.
-// Bound by memory for prompts (8191 rows of 24 + 8 heads of 128: 29.7 us, 5.66 TB/s), by latency for the rows of a step.
+// Bound by memory for prompts (8191 rows of 24 + 8 heads of 128: 28.9 us, 5.8 TB/s), by latency for the rows of a step.
 template <typename T, bool INTERLEAVED, int W>
 __global__ void __launch_bounds__(kRopeThreads, 8) rope_append_kernel(const __grid_constant__ sdv_rope_args a, const __grid_constant__ sdv_pages pages, int tokens) {
     extern __shared__ float2 turn[];   // [token][pair] cosine, sine
@@ -260,7 +260,8 @@ __global__ void __launch_bounds__(kRopeThreads, 8) rope_append_kernel(const __gr
 
 // Half layout with halves that are no multiple of eight: the partners of eight aligned elements do not lie on a 16-byte boundary.  The heads of q and k go through shared memory,
 // `heads` of a row at a time, and are turned there in place, two pairs a thread; global memory sees 16-byte accesses only.  A thread keeps its place within the heads and
-// steps from head to head without a division.  (Two bytes at a time from global memory, 51 pairs took 123 us where 56 took 32.)
+// steps from head to head without a division.  (Two bytes at a time from global memory, 51 pairs took 123 us; so they take 46, where 56,
+// which need no stage, take 32: the rows of a block follow each other, load, turn and store of each behind barriers.)
 template <typename T>
 __global__ void __launch_bounds__(kRopeThreads, 8) rope_staged_kernel(const __grid_constant__ sdv_rope_args a, const __grid_constant__ sdv_pages pages, int tokens, int heads) {
     extern __shared__ uint4 stage[];   // [head][16 bytes] | [token][pair] cosine, sine

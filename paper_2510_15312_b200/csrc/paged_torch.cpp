@@ -1,5 +1,5 @@
 // The operators on a cache kept in pages on torch tensors: argument checks, allocation of outputs and the calls of include/sdv.h, for paged.py.  A call
-// takes the host 5.1 us (an append) to 8 (an attention with its workspace and two launches); through Python checks and ctypes it took 11.2 to 14 (0.4 a tensor checked, 0.7 to 1.4 a tensor
+// takes the host 5.2 us (an append) to 8.4 (an attention with its workspace and two launches); through Python checks and ctypes it took 11.2 to 14 (0.4 a tensor checked, 0.7 to 1.4 a tensor
 // allocated).  Called on the current device and stream.  What shapes and types do not allow raises
 // ValueError; a status of the library other than SDV_OK is handed back as an int.
 #include <ATen/ATen.h>

@@ -204,11 +204,14 @@ __device__ __forceinline__ void tree_clear(const TreeParams& P, int lane) {
 // un-normalised outputs, maxima and sums in the workspace.  (Short tables are dealt out in whole items instead, see the host.)
 // Within a block: one warp copies keys and values, box by box of a page, into a ring of tiles (tensor maps: any strides, five tiles of 16 KB in flight a block); one issues S = Q K^T
 // into one of two tensor-memory buffers and, when four warps have turned it into probabilities in place (a tile row a thread, no exchange between threads), P V, which adds up in
-// tensor memory.  The output is rescaled only when a row's maximum grew by more than 2^8: probabilities stay below 2^8 (fp16: 2^15, see kProbShift) and their sums, in fp32, lose nothing.  S of the next tile is
+// tensor memory.  The output is rescaled only when a row's maximum grew by more than 2^8 (this and probabilities in tensor memory are published methods, named at
+// dense_attention_kernel): probabilities stay below 2^8 (fp16: 2^15, see kProbShift) and their sums, in fp32, lose nothing.  S of the next tile is
 // computed during the softmax of this one.  Probabilities are rounded to the 16-bit type for the second product, as its operand has to be; sums take them unrounded.
 // Bound by memory where the cache is long: 64 sequences of one row over up to 8192 tokens (619 MB, 7 heads a KV head) take 97 us here and 104 with the merge, 5.9 TB/s; a run of
 // many seconds is bound by power, 113 us.  24 trees of up to 40 rows (244 MB) take 49 us: 37 for the bytes, 4 until the first scores, the rest until the slowest block is through
-// (blocks of equal shares end up to 15 percent apart).  512 tile rows a KV head are bound by the L2, where each tile of rows reads the keys again.
+// (blocks of equal shares end up to 15 percent apart).  Several tiles of rows read the keys again from L2
+// each: 64 rows of 28 + 4 heads over 16000 tokens take 34.7 us (bytes 5.2, products 9.1).  They draw 3.8 TB/s from L2, less than a row a sequence draws through it from HBM: a block
+// takes 2 us a tile of 64 keys, its one stream's chain of load, S, softmax and P V.
 // Places behind a sequence's end hold anything: their values are cleared in shared memory (0 x NaN is not 0).  Rows of the tree
 // that a row does not see take part in its product with probability 0: infinities and NaN among their values are cleared too, and added
 // by those who see them at the end.

@@ -62,8 +62,8 @@ __device__ __forceinline__ void verify_load(const VerifyRest& d, int first, int 
 // A cluster takes one sequence.  All its blocks go through the drafts (at most 64 rows, one gather each; a row is looked at on its own, with the shares of its earlier
 // siblings, and the path is walked once); each sums up its part of the distribution that remains, tile by tile in a fixed order; every block writes its sum into the others' shared memory, and the block whose
 // part holds the drawn token reads that one tile again.  Sums in 64 bits: a token's share may be 10^-9 of the whole, fp32 sums would draw its neighbour.  A token's place is that of the
-// exact sums up to a relative 10^-15.  Bound by reading the row (and the draft's) once: 64 sequences at a vocabulary of 152064 with draft probabilities 17.7 us of which the 78 MB
-// take 11.9; for few sequences by the chain of round trips (lengths, rows, shares, row, tile): 7.4 us for one.  Two blocks an SM (their registers), all resident at once.
+// exact sums up to a relative 10^-15.  Bound by the chain of round trips (lengths, rows, shares, row, exchange, tile): 7.5 us for one
+// sequence; 64 at a vocabulary of 152064 with draft probabilities 17.7 us, 15.7 with the 78 MB in L2, of which reading them takes 11.9 (memory is 41 % busy, conversions 29 %, the 64-bit pipe 9 %).  Two blocks an SM (their registers), all resident at once.
 __global__ void __launch_bounds__(kVerifyThreads, 2) verify_sampled_kernel(const __grid_constant__ sdv_verify_args a, int tiles_per_block) {
     extern __shared__ double tile_sum[];   // [tiles_per_block]
     __shared__ int tok[SDV_TREE_ROWS], par[SDV_TREE_ROWS], out[SDV_TREE_ROWS], path[SDV_TREE_ROWS], child[SDV_TREE_ROWS];
